@@ -1,7 +1,7 @@
 """MI355X-native forward pass of one pipeline stage of decoder blocks.
 
 The work is done by the HIP library `libhyp_stage.so` (C ABI in
-include/hyp_stage.h); this package only marshals arguments.  Importing the
+include/hyp_stage.h, hyp_plan.h and hyp_attn.h); this package only marshals arguments.  Importing the
 package does not load the library; the first call does, and fails loudly if it
 has not been built (python -m paper_2511_14450_amd.build).
 """
@@ -11,6 +11,9 @@ from .binding import (  # noqa: F401
     stage_last_error, stage_prefill, stage_set_page_table, stage_profile, stage_profile_read, stage_uses_mfma,
     stage_workspace_bytes, KERNEL_CLASSES, stage_config, hyp_measure_mfma_ceiling,
     hyp_measure_hbm_read_ceiling, hypsplit_dp, hypsched_rt, hypsched_simulate,
+)
+from .attn import (  # noqa: F401
+    AttnCache, AttnRule, attn_evict, attn_last_error, attn_prompt, attn_received, attn_token, attn_workspace_bytes,
 )
 
 

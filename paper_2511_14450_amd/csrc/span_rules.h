@@ -1,0 +1,35 @@
+// How a call of hyp_attn.h is cut into workgroups.  Plain C++, so that it can be checked on the host.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+namespace hyp {
+
+// attn_prompt: parts that the keys of a row tile are cut into.  Without a cut a tile's workgroup meets all its keys; that fills the
+// chip from one workgroup a CU on.
+inline int span_prompt_splits(int64_t workgroups, int64_t stages) {
+  if (workgroups >= 256 || stages < 8) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(workgroups, 1), stages / 4, 64}));
+}
+
+struct SpanTokenPlan { int pre_wide, pre_tiles, pre_splits, tiles, splits; };
+
+// attn_token: waves: of a workgroup; pre_stage: keys of a stage of items over the shared keys where each wave has rows of its own
+inline SpanTokenPlan span_token_plan(int64_t requests, int64_t kv_heads, int64_t group, int64_t most, int64_t prefix, int waves, int pre_stage) {
+  SpanTokenPlan t = {};
+  const int64_t rows = requests * group;
+  t.tiles = (int)((group + 31) / 32);
+  t.pre_wide = rows > 32;
+  const int64_t tile = t.pre_wide ? 32 * waves : 32;
+  t.pre_tiles = prefix ? (int)((rows + tile - 1) / tile) : 0;
+  const int64_t own_items = requests * kv_heads * t.tiles, pre_items = (int64_t)t.pre_tiles * kv_heads;
+  const int64_t keys = own_items * most + pre_items * prefix;
+  const int64_t part = std::max<int64_t>((keys + 511) / 512, 256);
+  auto cut = [&](int64_t n, int64_t stage) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + part - 1) / part, (n + stage - 1) / stage)); };
+  t.splits = cut(most, 32 * waves);
+  t.pre_splits = prefix ? cut(prefix, t.pre_wide ? pre_stage : 32 * waves) : 0;
+  return t;
+}
+
+}  // namespace hyp
