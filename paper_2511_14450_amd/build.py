@@ -22,7 +22,7 @@ FLAGS = [
 
 
 # per-file additions: the attention kernels take maxima over MFMA results that are never NaN
-EXTRA_FLAGS = {"mfma_attention.hip": ["-fno-honor-nans"]}
+EXTRA_FLAGS = {name: ["-fno-honor-nans"] for name in ("mfma_attention.hip", "span_bf16.hip", "span_f32.hip")}
 
 
 def _newest_header() -> float:

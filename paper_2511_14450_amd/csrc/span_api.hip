@@ -109,6 +109,13 @@ void add_rule(SpanCall &p, const hyp_attn_rule_t &rule) {
   if (rule.cap > 0.f) {
     p.to_cap = rule.scale / rule.cap;
     p.cap2 = rule.cap * log2e;
+    // tanh(x) / x in powers of x^2
+    constexpr double tanh_c[6] = {1.0, -0.3333328366279602, 0.13331490755081177, -0.05374349653720856, 0.020650586113333702, -0.005717044696211815};
+    const double k = (double)rule.scale / rule.cap;
+    double f = (double)rule.scale * log2e;
+    for (int i = 0; i < 6; ++i, f *= k * k) p.cap_c[i] = (float)(f * tanh_c[i]);
+    p.cap_most = (float)(0.625 / k);
+    if (!std::isfinite(p.cap_c[5])) p.cap_most = -1.f;  // a cap below 1e-4 of the scale: tanh is 0 or 1, the polynomial is not used
   }
   p.slopes = rule.slopes;
 }

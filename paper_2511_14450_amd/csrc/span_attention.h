@@ -31,7 +31,16 @@ __device__ __forceinline__ float half_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+// This file is compiled as if no number were NaN, so that a maximum is one instruction.  Where a NaN may stand it is looked at
+// as an integer, which the compiler is kept from seeing through.
+__device__ __forceinline__ unsigned bits_of(float x) {
+  unsigned u = __float_as_uint(x);
+  asm("" : "+v"(u));
+  return u;
+}
+__device__ __forceinline__ bool not_finite(float x) { return (bits_of(x) & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool is_zero(float x) { return bits_of(x) == 0u; }
+__device__ __forceinline__ bool is_none(float x) { return bits_of(x) == 0xff800000u; }  // the maximum of no score
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) v = min(v, __shfl_xor(v, s));
@@ -40,37 +49,21 @@ __device__ __forceinline__ int wave_min(int v) {
 __device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
 __device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-// A raw score as an exponent of two, cap * log2(e) * tanh(s scale / cap).  |x| <= 0.625: x + x^3 Q(x^2), Q fitted to an even
-// relative error (4e-9; 7e-8 as evaluated); beyond, 1 - 2 / (e^2x + 1), whose absolute error of one rounding is relative there.
-__device__ __forceinline__ float cap_small(float x, float cap2) {
-  const float y = x * x, w = x * cap2;
-  float q = fmaf(y, -0.005717044696211815f, 0.020650586113333702f);
-  q = fmaf(y, q, -0.05374349653720856f);
-  q = fmaf(y, q, 0.13331490755081177f);
-  q = fmaf(y, q, -0.3333328366279602f);
-  return fmaf(w * y, q, w);
+// A raw score S as an exponent of two, cap log2(e) tanh(S scale / cap).  With x = S scale / cap up to 0.625 in absolute value that is
+// S r(S^2), r a polynomial fitted to an even relative error (4e-9; 1e-7 as evaluated), whose coefficients the host scales;
+// beyond, 1 - 2 / (e^2x + 1), whose absolute error of one rounding is relative there.
+__device__ __forceinline__ float cap_factor(float s, const float (&c)[6]) {
+  const float y = s * s;
+  float q = fmaf(y, c[5], c[4]);
+  q = fmaf(y, q, c[3]);
+  q = fmaf(y, q, c[2]);
+  q = fmaf(y, q, c[1]);
+  return fmaf(y, q, c[0]);
 }
-__device__ __forceinline__ float cap_large(float x, float cap2) {
-  const float e = exp2_(2.0f * kLog2e * fabsf(x));  // infinity: tanh is 1
-  return copysignf(cap2 - 2.0f * cap2 * __builtin_amdgcn_rcpf(e + 1.0f), x);
-}
-template <int N> __device__ __forceinline__ void cap_scores(float (&s)[N], float to_cap, float cap2) {
-  float top = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    s[i] *= to_cap;
-    top = fmaxf(top, fabsf(s[i]));
-  }
-  if (!__any(!(top <= 0.625f))) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = cap_small(s[i], cap2);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float a = cap_small(s[i], cap2), b = cap_large(s[i], cap2);
-      s[i] = fabsf(s[i]) <= 0.625f ? a : b;
-    }
-  }
+__device__ __forceinline__ float cap_any(float s, const float (&c)[6], float most, float to_cap, float cap2) {
+  const float e = exp2_(2.0f * kLog2e * fabsf(s * to_cap));  // infinity: tanh is 1
+  const float far = copysignf(cap2 - 2.0f * cap2 * __builtin_amdgcn_rcpf(e + 1.0f), s);
+  return fabsf(s) <= most ? s * cap_factor(s, c) : far;
 }
 
 __device__ __forceinline__ float load_val(const float *p) { return *p; }
@@ -135,12 +128,14 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
   static constexpr int LDS_ALL = LDS > JOIN ? LDS : JOIN;
   static_assert(LDS_ALL <= 160 * 1024, "LDS of a CU");
 
-  // Rows of 8 pieces fill half the banks: an exchange of pieces by the row lets 32 rows be read at one piece, and four rows of
-  // values at two, without two lanes meeting in a bank.
-  static __device__ __forceinline__ int kswz(int row) { return row & 7; }
+  // LDS has 64 banks of 4 bytes: rows of 16 pieces or more fill them all, rows of 8 half of them.  The pieces of a row are exchanged by the
+  // row's number, so that the 16 rows that 16 lanes read a piece of, and the two pieces of four value rows that 32 lanes read, meet in
+  // no bank.
+  static constexpr int KM = CPR >= 16 ? 15 : 7;
+  static __device__ __forceinline__ int kswz(int row) { return row & KM; }
   static __device__ __forceinline__ int vswz(int row) {
     if constexpr (ES == 4) return ((row >> 2) & 1) << 3;
-    return (row & (CPR >= 16 ? 7 : 3)) << 1;
+    return CPR >= 16 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
   }
 
   const SpanCall &p;
@@ -195,7 +190,7 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
       const bool one_page = s.base + SKEYS <= s.end && !(s.own && small_page);
       if (one_page) {
         const T *start = base + offset(s.base);
-        constexpr int SAME = ROWS % 8 == 0;
+        constexpr bool SAME = ROWS % (KM + 1) == 0;  // all of a lane's rows exchange alike
         const unsigned step = (unsigned)(ROWS * ks * ES);
         const int c0 = piece ^ (VALUES ? vswz(first) : kswz(first));
         const unsigned off0 = (unsigned)(first * ks * ES) + c0 * 16;
@@ -301,8 +296,10 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
 
   // cap and bias of one block of 32 keys from `base` on; kpos: positions of its keys in LDS, or null
   __device__ __forceinline__ void rule(float (&s)[16], const SpanRow &r, int first_pos, const int *kpos) const {
-    if (p.cap2 != 0.f) cap_scores(s, p.to_cap, p.cap2);
-    else {
+    if (p.cap2 != 0.f) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = cap_any(s[i], p.cap_c, p.cap_most, p.to_cap, p.cap2);
+    } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] *= p.scale2;
     }
@@ -344,40 +341,64 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
     float s[NKB][16];
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb) block_scores(keys + kb * 32 * ROWB, rows, col, hh, s[kb]);
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-      rule(s[kb], r, (sta.own ? p.c.prefix_len : 0) + base + kb * 32, sta.own && has_pos ? ints + SKEYS + kb * 32 : nullptr);
-    if (edge) {
-      const int last = sta.own ? min(r.lim, sta.end - 1) : sta.end - 1;
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (base + kb * 32 + key_of(i, hh) > last) s[kb][i] = -INFINITY;
-    }
-    if (docs) {
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const i32x4_t id = *(const i32x4_t *)(ints + kb * 32 + 8 * g + 4 * hh);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (id[e] != r.doc && id[e] >= 0 && r.doc >= 0) s[kb][4 * g + e] = -INFINITY;
-        }
-    }
-    if (score_out && sta.own && r.there) {
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)  // up to the row's pitch, a multiple of the stage
-          *(f32x4_t *)(score_out + base + kb * 32 + 8 * g + 4 * hh) = f32x4_t{s[kb][4 * g], s[kb][4 * g + 1], s[kb][4 * g + 2], s[kb][4 * g + 3]};
-    }
+    // Scores that all rows see and that no distance moves stay raw: cap and scale do not change their order, so the maximum is
+    // taken of them as they are, and the last step of either is one instruction with the subtraction of the maximum.
+    const bool capped = p.cap2 != 0.f;
+    bool raw = !(edge || docs || p.slopes || score_out);
     float mx = -INFINITY;
+    if (raw) {
 #pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
+      for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[kb][i]), s[kb][i + 1]);
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[kb][i]), s[kb][i + 1]);
+      if (capped) {
+        float far = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) far = fmaxf(fmaxf(far, fabsf(s[kb][i])), fabsf(s[kb][i + 1]));
+        raw = !__any(!(far <= p.cap_most));
+        mx *= cap_factor(mx, p.cap_c);
+      } else {
+        mx *= p.scale2;
+      }
+    }
+    if (!raw) {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+        rule(s[kb], r, (sta.own ? p.c.prefix_len : 0) + base + kb * 32, sta.own && has_pos ? ints + SKEYS + kb * 32 : nullptr);
+      if (edge) {
+        const int last = sta.own ? min(r.lim, sta.end - 1) : sta.end - 1;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (base + kb * 32 + key_of(i, hh) > last) s[kb][i] = -INFINITY;
+      }
+      if (docs) {
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const i32x4_t id = *(const i32x4_t *)(ints + kb * 32 + 8 * g + 4 * hh);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (id[e] != r.doc && id[e] >= 0 && r.doc >= 0) s[kb][4 * g + e] = -INFINITY;
+          }
+      }
+      if (score_out && sta.own && r.there) {
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)  // up to the row's pitch, a multiple of the stage
+            *(f32x4_t *)(score_out + base + kb * 32 + 8 * g + 4 * hh) = f32x4_t{s[kb][4 * g], s[kb][4 * g + 1], s[kb][4 * g + 2], s[kb][4 * g + 3]};
+      }
+      mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[kb][i]), s[kb][i + 1]);
+    }
     const float m_new = fmaxf(t.m, half_max(mx));
     if (__any(m_new - t.m > kFollow)) {
       const float alpha = m_new == -INFINITY ? 1.0f : exp2_(t.m - m_new);
@@ -389,14 +410,23 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
       t.m = m_new;
     }
     const float m = t.m == -INFINITY ? 0.f : t.m;  // a row that has seen nothing yet: all its probabilities are 2^-inf
+    if (raw && capped) {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = exp2_(fmaf(s[kb][i], cap_factor(s[kb][i], p.cap_c), -m));
+    } else {
+      const float c = raw ? p.scale2 : 1.0f;
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = exp2_(fmaf(s[kb][i], c, -m));
+    }
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb) {
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[kb][i] = exp2_(s[kb][i] - m);
-        sum += s[kb][i];
-      }
+      for (int i = 0; i < 16; ++i) sum += s[kb][i];
       t.l += sum;
     }
 #pragma unroll
@@ -439,7 +469,7 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
   // their final weights, from memory.  Slow, and right.  The result is the one of a sum of one.
   __device__ __forceinline__ void careful(int st0, int st1, const SpanRow &r, State &t) const {
     const int kw = KW > 1 ? wave / RW : 0, d = p.c.head_dim;
-    if (t.l != 0.f) {
+    if (!is_zero(t.l)) {
       t.m += __builtin_amdgcn_logf(t.l);
       t.l = 1.0f;
     }
@@ -468,19 +498,14 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
           ko = sg.kvh * p.c.prefix_k_head_stride + key * p.c.prefix_k_key_stride;
           vo = sg.kvh * p.c.prefix_v_head_stride + key * p.c.prefix_v_key_stride;
         }
-        if (!seen || t.l == 0.f) continue;
+        if (!seen || is_zero(t.l)) continue;
         const T *k = (const T *)(sta.own ? p.c.k : p.c.prefix_k) + ko, *v = (const T *)(sta.own ? p.c.v : p.c.prefix_v) + vo;
-        float dot[1] = {0.f};
-        for (int f = 0; f < d; ++f) dot[0] = fmaf(load_val((const T *)r.q + f), load_val(k + f), dot[0]);
-        if (p.cap2 != 0.f) {
-          const float x = dot[0] * p.to_cap;
-          dot[0] = fabsf(x) <= 0.625f ? cap_small(x, p.cap2) : cap_large(x, p.cap2);
-        } else {
-          dot[0] *= p.scale2;
-        }
-        if (p.slopes) dot[0] -= r.slope2 * fabsf((float)(r.pos - pos));
-        const float pr = exp2_(dot[0] - m);
-        if (pr == 0.f) continue;
+        float dot = 0.f;
+        for (int f = 0; f < d; ++f) dot = fmaf(load_val((const T *)r.q + f), load_val(k + f), dot);
+        dot = p.cap2 != 0.f ? cap_any(dot, p.cap_c, p.cap_most, p.to_cap, p.cap2) : dot * p.scale2;
+        if (p.slopes) dot -= r.slope2 * fabsf((float)(r.pos - pos));
+        const float pr = exp2_(dot - m);
+        if (is_zero(pr)) continue;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -521,7 +546,7 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
   __device__ __forceinline__ void store_rows(const SpanRow &r, const State &t, int slot) const {
     if (!r.there) return;
     const int d = p.c.head_dim;
-    const bool none = t.l == 0.f;
+    const bool none = is_zero(t.l);
     const float inv = none ? 0.f : 1.0f / t.l;
     if (p.part_o) {
       const int64_t at = (int64_t)slot * p.n_rows * p.nq + r.at;
@@ -584,7 +609,7 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[64 + (32 * db + key_of(i, hh)) * 33 + col] = t.o[db][i];
     if (hh == 0) {
-      mine[col] = t.l == 0.f ? -INFINITY : t.m;
+      mine[col] = is_zero(t.l) ? -INFINITY : t.m;
       mine[32 + col] = t.l;
     }
     __syncthreads();
@@ -598,25 +623,25 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float *x = (float *)lds + w * PER;
-        a[w] = x[row] == -INFINITY ? 0.f : exp2_(x[row] - m);
-        if (a[w] != 0.f) l += a[w] * x[32 + row];
+        a[w] = is_none(x[row]) ? 0.f : exp2_(x[row] - m);
+        if (!is_zero(a[w])) l += a[w] * x[32 + row];
       }
       const float inv = 1.0f / l;
 #pragma unroll
       for (int w = 0; w < KW; ++w)
-        if (a[w] != 0.f) o += a[w] * inv * ((float *)lds)[w * PER + 64 + f * 33 + row];
+        if (!is_zero(a[w])) o += a[w] * inv * ((float *)lds)[w * PER + 64 + f * 33 + row];
       const int64_t pair = pair_at(p, first, sg.kvh, row), r = pair / p.nq;
       const int head = (int)(pair - r * p.nq);
       if (p.part_o) {
         const int64_t to = (int64_t)slot * p.n_rows * p.nq + pair;
         p.part_o[to * d + f] = o;
         if (f == 0) {
-          p.part_ml[2 * to] = l == 0.f ? -INFINITY : m;
+          p.part_ml[2 * to] = is_zero(l) ? -INFINITY : m;
           p.part_ml[2 * to + 1] = l;
         }
       } else {
         store_f32((T *)p.out + r * p.out_rs + head * p.out_hs + f, o);
-        if (f == 0 && p.lse) p.lse[pair] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        if (f == 0 && p.lse) p.lse[pair] = is_zero(l) ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
       }
     }
   }
@@ -642,7 +667,7 @@ __device__ __forceinline__ int64_t tile_request(const SpanCall &p, int t, int ti
 
 // attn_prompt.  A workgroup: one KV head, 128 rows of one request (dense over the group's heads), all the keys they see or one
 // of `splits` parts of them.
-template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * kSpanWaves) k_span_prompt(const SpanCall p) {
+template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_prompt(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), WIDE>;
   int id = blockIdx.x;
@@ -732,7 +757,7 @@ __device__ __forceinline__ float2 slots_total(const SpanCall &p, int slots, int6
   float l = 0.f;
   for (int s = lane; s < slots; s += 64) {
     const float ms = p.part_ml[2 * (s * all + pair)];
-    if (ms != -INFINITY) l += exp2_(ms - m) * p.part_ml[2 * (s * all + pair) + 1];
+    if (!is_none(ms)) l += exp2_(ms - m) * p.part_ml[2 * (s * all + pair) + 1];
   }
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
@@ -752,13 +777,13 @@ template <typename T> __global__ void __launch_bounds__(256) k_span_join(const S
     const float2 ml = slots_total(p, slots, pair, lane);
     const int head = (int)(pair - row * p.nq);
     T *out = (T *)p.out + row * p.out_rs + head * p.out_hs;
-    const bool none = ml.x == -INFINITY;
+    const bool none = is_none(ml.x);
     if (p.lse && lane == 0) p.lse[pair] = none ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2;
     const float inv = none ? 0.f : 1.0f / ml.y;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < slots; ++s) {
       const float ms = p.part_ml[2 * (s * all + pair)];
-      if (ms == -INFINITY) continue;
+      if (is_none(ms)) continue;
       const float a = exp2_(ms - ml.x) * p.part_ml[2 * (s * all + pair) + 1] * inv;
       const float *o = p.part_o + (s * all + pair) * d;
 #pragma unroll
@@ -782,7 +807,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_span_join(const S
   if (kb * 1024 < len) {
     for (int g = wave; g < p.G; g += 4) {
       const float2 ml = slots_total(p, slots, (int64_t)b * p.nq + kvh * p.G + g, lane);
-      if (lane == 0) lse2[g] = ml.x == -INFINITY ? INFINITY : ml.x + __builtin_amdgcn_logf(ml.y);
+      if (lane == 0) lse2[g] = is_none(ml.x) ? INFINITY : ml.x + __builtin_amdgcn_logf(ml.y);
     }
   }
   __syncthreads();
@@ -872,7 +897,7 @@ template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(256) 
     Info x;
     x.r = span_row<T>(p, row, head_of(there ? pair : 0), b, len - n + (int)(row - row0), there);
     const float lse = there ? p.lse_in[x.r.at] : -INFINITY;
-    x.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    x.lse2 = is_none(lse) ? INFINITY : lse * kLog2e;
     return x;
   };
   float acc[16];
@@ -907,8 +932,10 @@ template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(256) 
     float s[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = a[i];
-    if (p.cap2 != 0.f) cap_scores(s, p.to_cap, p.cap2);
-    else {
+    if (p.cap2 != 0.f) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = cap_any(s[i], p.cap_c, p.cap_most, p.to_cap, p.cap2);
+    } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] *= p.scale2;
     }

@@ -14,6 +14,7 @@ struct SpanCall {
   int G, nq;
   float scale2;               // scale * log2(e): scores are held as exponents of two
   float to_cap, cap2;         // scale / cap, cap * log2(e); cap2 0: not capped
+  float cap_c[6], cap_most;   // polynomial of the capped score, and the largest raw score it is for
   const float *slopes;
   const void *q;
   int64_t q_rs, q_hs;
@@ -59,6 +60,7 @@ __host__ __device__ constexpr int span_steps(int d, bool wide) { return !wide ? 
 __host__ __device__ constexpr int span_chunks(int nt, int es) { return (nt == 6 ? 8 : nt) * es; }                 // 16-byte pieces of an LDS row
 __host__ __device__ constexpr int span_stage_keys(int nt, int es) { return es == 2 && nt <= 8 ? 64 : 32; }        // a wave's keys of a stage, waves by rows
 __host__ __device__ constexpr int span_token_waves(int nt, int es) { return span_chunks(nt, es) <= 16 ? 4 : span_chunks(nt, es) <= 32 ? 2 : 1; }
+__host__ __device__ constexpr int span_steps_waves(int nt) { return nt <= 8 ? 2 : 1; }  // waves a SIMD that the registers are shared out for
 constexpr int kSpanWaves = 4;          // attn_prompt: waves of 32 rows
 constexpr int kSpanTile = 32 * kSpanWaves;
 constexpr int kSpanReceivedKeys = 128; // keys of a workgroup of attn_received
