@@ -110,12 +110,12 @@ void add_rule(SpanCall &p, const hyp_attn_rule_t &rule) {
     p.to_cap = rule.scale / rule.cap;
     p.cap2 = rule.cap * log2e;
     // tanh(x) / x in powers of x^2
-    constexpr double tanh_c[6] = {1.0, -0.3333328366279602, 0.13331490755081177, -0.05374349653720856, 0.020650586113333702, -0.005717044696211815};
+    constexpr double tanh_c[5] = {1.0, -0.33333149552345276, 0.1332598775625229, -0.05305295065045357, 0.01725699193775654};
     const double k = (double)rule.scale / rule.cap;
     double f = (double)rule.scale * log2e;
-    for (int i = 0; i < 6; ++i, f *= k * k) p.cap_c[i] = (float)(f * tanh_c[i]);
-    p.cap_most = (float)(0.625 / k);
-    if (!std::isfinite(p.cap_c[5])) p.cap_most = -1.f;  // a cap below 1e-4 of the scale: tanh is 0 or 1, the polynomial is not used
+    for (int i = 0; i < 5; ++i, f *= k * k) p.cap_c[i] = (float)(f * tanh_c[i]);
+    p.cap_most = (float)(0.5 / k);
+    if (!std::isfinite(p.cap_c[4])) p.cap_most = -1.f;  // a cap below 1e-4 of the scale: tanh is 0 or 1, the polynomial is not used
   }
   p.slopes = rule.slopes;
 }
@@ -143,7 +143,7 @@ Plan plan_prompt(SpanCall &p, bool wide) {
   const int64_t stages = (p.c.prefix_len + stage - 1) / stage + (p.c.most + stage - 1) / stage;
   p.tiles = (int)tiles;
   p.splits = span_prompt_splits(tiles * p.c.n_kv_heads, stages);
-  need(tiles * p.splits * p.c.n_kv_heads < (1ll << 31), HYP_ESHAPE, "too many row tiles for a launch");
+  need(tiles * p.splits * (p.c.n_kv_heads + 8) < (1ll << 31), HYP_ESHAPE, "too many row tiles for a launch");
   Plan w;
   if (p.splits > 1) {
     w.part_o = (int64_t)p.splits * p.n_rows * p.nq * p.c.head_dim;

@@ -1,0 +1,77 @@
+// Which stages of its keys a workgroup of attn_prompt goes through where keys and rows have ids.
+//
+// Documents lie side by side in a request, and a tile's rows mostly belong to one: a look at the ids first leaves out the stages that hold
+// nothing for them, and the masks of those that hold nothing else.
+#pragma once
+
+#include "span_core.h"
+
+namespace hyp {
+namespace {
+
+constexpr int kLiveWords = 256;  // 32 stages a word: beyond 8192 stages (half a million keys in stages of 64) all are gone through
+
+template <typename S> struct Survey {
+  static constexpr int LDS = 2 * kLiveWords * 4 + 16;
+  const S &span;
+  const unsigned *live;  // bits of own stages: holds a key that some row may see; then of those that hold one that some row may not
+  bool masks;
+
+  __device__ __forceinline__ Survey(const S &s, char *lds, const SpanRow &r) : span(s), live((const unsigned *)lds), masks(s.has_doc) {
+    if (!masks) return;
+    unsigned *bits = (unsigned *)lds;
+    int *range = (int *)(lds + 2 * kLiveWords * 4);
+    if (threadIdx.x == 0) {
+      range[0] = 0x7fffffff;
+      range[1] = -0x7fffffff;
+    }
+    for (int i = threadIdx.x; i < 2 * kLiveWords; i += S::THREADS) bits[i] = 0;
+    __syncthreads();
+    const int lo = wave_min(r.there ? r.doc : 0x7fffffff), hi = wave_max(r.there ? r.doc : -0x7fffffff);
+    if (span.lane == 0) {
+      atomicMin(&range[0], lo);
+      atomicMax(&range[1], hi);
+    }
+    __syncthreads();
+    const int low = range[0], high = range[1];  // low < 0: some row sees every id; high < 0: all do
+    const int *docs = span.p.c.key_doc + span.sg.req * span.p.c.key_doc_request_stride + span.sg.kvh * span.p.c.key_doc_head_stride;
+    const int count = min(span.stages - span.pre_stages, 32 * kLiveWords);
+    for (int i = span.wave; i < count; i += S::NW) {
+      bool seen = false, hides = false;
+#pragma unroll
+      for (int x = 0; x < (S::SKEYS + 63) / 64; ++x) {
+        const int id = docs[min(span.sg.b0 + i * S::SKEYS + x * 64 + min(span.lane, S::SKEYS - 1), span.sg.b1 - 1)];
+        seen |= id < 0 || low < 0 || (id >= low && id <= high);
+        hides |= !(id < 0 || high < 0 || (low == high && id == low));
+      }
+      const bool any_seen = __any(seen), any_hides = __any(hides);
+      if (span.lane == 0) {
+        if (any_seen) atomicOr(&bits[i >> 5], 1u << (i & 31));
+        if (any_hides) atomicOr(&bits[kLiveWords + (i >> 5)], 1u << (i & 31));
+      }
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ int next(int st, int st1) const {
+    if (!masks) return min(st, st1);
+    while (st < st1 && st >= span.pre_stages && st - span.pre_stages < 32 * kLiveWords) {
+      const int i = st - span.pre_stages;
+      const unsigned left = __builtin_amdgcn_readfirstlane(live[i >> 5]) >> (i & 31);
+      if (left) {
+        st += __builtin_ctz(left);
+        break;
+      }
+      st += 32 - (i & 31);
+    }
+    return min(st, st1);
+  }
+  __device__ __forceinline__ bool hides(int st) const {
+    const int i = st - span.pre_stages;
+    if (!masks || i < 0) return false;
+    if (i >= 32 * kLiveWords) return true;
+    return (__builtin_amdgcn_readfirstlane(live[kLiveWords + (i >> 5)]) >> (i & 31)) & 1;
+  }
+};
+
+}  // namespace
+}  // namespace hyp
