@@ -91,6 +91,9 @@ SpanCall begin(const hyp_attn_cache_t &c, const hyp_attn_rows_t &r) {
   p.page_shift = shift_of(c);
   p.nq = r.n_q_heads;
   p.G = r.n_q_heads / c.n_kv_heads;
+  p.g_shift = -1;
+  for (int s = 0; s < 9; ++s)
+    if (p.G == 1 << s) p.g_shift = s;
   p.q = r.q;
   p.q_rs = r.q_row_stride;
   p.q_hs = r.q_head_stride;
@@ -290,7 +293,9 @@ hyp_status_t attn_received(const hyp_attn_cache_t *cache, const hyp_attn_rule_t 
     p.lse_in = lse;
     p.last = last;
     const bool wide = is_wide(*cache, *rows);
-    const int64_t blocks = (int64_t)((p.c.most + kSpanReceivedKeys - 1) / kSpanReceivedKeys) * p.c.n_requests * p.c.n_kv_heads;
+    // causality gives the first keys the most rows; with few rows to meet it is the keys that take the time, and more workgroups fetch them
+    p.pairs_of_blocks = last == 0 || (int64_t)last * p.G > 512;
+    const int64_t blocks = (int64_t)((p.c.most + 63) / 64) * p.c.n_requests * (p.c.n_kv_heads + 8);
     need(blocks < (1ll << 31), HYP_ESHAPE, "too many keys for a launch");
     const hipStream_t s = (hipStream_t)hip_stream;
     run(p.c.dtype == HYP_BF16 ? span_received<bf16_t>(p, wide, s) : span_received<float>(p, wide, s));

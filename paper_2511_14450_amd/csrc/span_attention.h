@@ -203,142 +203,255 @@ template <typename T> __global__ void __launch_bounds__(256) k_span_join(const S
   }
 }
 
-// attn_received.  A workgroup: one KV head and 128 own keys of a request, 32 a wave, which stay in registers; the rows that see
-// them pass by in tiles of 32 through LDS, as the keys do above.
-template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(256) k_span_received(const SpanCall p) {
+// attn_received.  A workgroup: a block of own keys of a request and KV head, 64 KB of them, or one from the front and one from the back, so
+// that all workgroups have about the same number of rows to meet.  Half of its NW waves hold one half of the keys in registers, half the
+// other; a head's rows pass by through LDS, ROWS at a time, from the last to the first, so that the workgroups of an XCD meet the same rows
+// at about the same time.  What a key gets is summed in its lane over the rows, then over lanes and waves, in a fixed order.
+// Rows come from L2 for every block of keys: 64 keys of 128 bf16 features to a block made that the bound (4.5 TB/s).
+template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> struct Received {
+  using S = Span<T, NT, NW, 1, 32, WIDE>;
+  static constexpr int ES = sizeof(T), EPC = 16 / ES, KEYS = 64 * KB, THREADS = 64 * NW, TILE = ROWS * S::ROWB;
+  static constexpr int SHARE = ((NW / 2) * KEYS * 4 + 2 * KEYS * 4 + 1023) / 1024 * 1024, LDS_ONE = SHARE + TILE, LDS = LDS_ONE + TILE;
+  static constexpr int LOADS = ROWS * S::CPR / THREADS, STEP = THREADS / S::CPR;  // a lane's loads of a stage, and the rows between them
+  static constexpr int TILES = ROWS / 32 / (NW / 2);                              // of a wave in a stage
+  static_assert(LOADS * THREADS == ROWS * S::CPR && TILES >= 1 && LDS <= 160 * 1024, "a stage is whole loads of all waves, and whole tiles");
+
+  const SpanCall &p;
+  S span;
+  char *lds;
+  int wave, lane, hh, col, kvh, b, len, n, from, pairs, all;
+  int64_t row0;
+
+  __device__ __forceinline__ Received(const SpanCall &p_, char *lds_, int kvh_, int b_, int len_)
+      : p(p_), span(p_, SpanKeys{0, 0, 0, len_, b_, kvh_}, lds_), lds(lds_), kvh(kvh_), b(b_), len(len_) {
+    wave = span.wave; lane = span.lane; hh = span.hh; col = span.col;
+    row0 = uniform((int)min(max((int64_t)p.q_start[b], (int64_t)0), p.n_rows));
+    const int64_t row1 = uniform((int)max(min((int64_t)p.q_start[b + 1], p.n_rows), row0));
+    n = (int)(row1 - row0);
+    all = p.see_all ? clamped(uniform(p.see_all[b]), 0, len) : 0;
+  }
+  __device__ __forceinline__ void place(int pair, int &row, int &head) const {  // of a pair of the rows that count
+    const int r = p.g_shift >= 0 ? pair >> p.g_shift : pair / p.G;
+    row = (int)row0 + from + r;
+    head = kvh * p.G + pair - r * p.G;
+  }
+
+  // What a lane knows of its row, as it comes from memory: looked at a stage later, or it would be waited for at once.
+  struct Info {
+    int doc, pos;
+    float lse, slope;
+  };
+  __device__ __forceinline__ Info info(int pair) const {
+    int row, head;
+    place(min(pair, pairs - 1), row, head);
+    Info x = {-1, 0, p.lse_in[(int64_t)row * p.nq + head], 0.f};
+    if (p.c.key_doc) x.doc = p.q_doc[row];
+    if (p.slopes) {
+      x.slope = p.slopes[head];
+      if (p.q_pos) x.pos = p.q_pos[row];
+    }
+    return x;
+  }
+
+  __device__ __forceinline__ void block(int key0, const float *in, float *out) {
+    from = p.last > 0 ? max(0, n - p.last) : 0;                  // the first row that counts
+    if (key0 >= all) from = max(from, key0 - (len - n));         // rows before it see none of these keys
+    const int mine = key0 + (int)threadIdx.x;                    // the key whose total this thread adds up at the end
+    const bool adds = threadIdx.x < KEYS && mine < p.c.most;
+    const float before = adds ? in[mine] : 0.f;
+    if (key0 >= len || from >= n) {
+      if (adds) out[mine] = before;
+      return;
+    }
+    pairs = (n - from) * p.G;
+    const int kw = wave & 1, rw = wave >> 1, my_key0 = key0 + 32 * KB * kw;
+    typename S::Rows keys[KB];
+    const bool has_doc = p.c.key_doc != nullptr;
+    // where this lane's pieces of a stage of rows come from; a whole stage before, the same pieces lie a fixed step back if the heads divide it
+    const char *at[LOADS];
+    const bool even = p.g_shift >= 0 && p.G <= ROWS;
+    const int64_t step = even ? (int64_t)(ROWS >> p.g_shift) * p.q_rs * ES : 0;
+    const int stages = (pairs + ROWS - 1) / ROWS;
+    auto issue = [&](int s) {  // the s-th from the end
+      char *dst = lds + SHARE + (s & 1) * TILE;
+      const int pair0 = (stages - 1 - s) * ROWS;
+      if constexpr (WIDE) {
+        const int first = threadIdx.x / S::CPR, piece = threadIdx.x % S::CPR;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const int r = first + j * STEP, c = piece ^ S::kswz(r);
+          if (even && s >= 2) at[j] -= step;
+          else {
+            int row, head;
+            place(min(pair0 + r, pairs - 1), row, head);
+            at[j] = (const char *)((const T *)p.q + row * p.q_rs + head * p.q_hs) + c * 16;
+          }
+          if (c < span.chunks) __builtin_amdgcn_global_load_lds((gbl_ptr_t *)at[j], (lds_ptr_t *)(dst + (j * NW + wave) * 1024), 16, 0, 0);
+        }
+      } else {
+        const int d = p.c.head_dim;
+        for (int i = threadIdx.x; i < ROWS * d; i += THREADS) {
+          const int r = i / d, f = i % d, c = (f / EPC) ^ S::kswz(r);
+          int row, head;
+          place(min(pair0 + r, pairs - 1), row, head);
+          ((T *)(dst + r * S::ROWB + c * 16))[f % EPC] = ((const T *)p.q)[row * p.q_rs + head * p.q_hs + f];
+        }
+      }
+    };
+    __syncthreads();  // the block before is done with LDS
+    issue(0);
+    if (threadIdx.x < KEYS) {  // ids and positions of the keys, for the rows that want them
+      int *ints = (int *)lds + (NW / 2) * KEYS;
+      const int key = min(mine, len - 1);
+      if (has_doc) ints[threadIdx.x] = p.c.key_doc[b * p.c.key_doc_request_stride + kvh * p.c.key_doc_head_stride + key];
+      if (p.slopes) ints[KEYS + threadIdx.x] = p.c.key_pos ? p.c.key_pos[b * p.c.key_pos_request_stride + kvh * p.c.key_pos_head_stride + key] : p.c.prefix_len + key;
+    }
+    Info next[TILES];
+#pragma unroll
+    for (int x = 0; x < TILES; ++x) next[x] = info((stages - 1) * ROWS + (x * (NW / 2) + rw) * 32 + col);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int first = my_key0 + 32 * kb;
+      span.load_row((const T *)p.c.k + own_offset(p.c, p.page_shift, p.c.k_page_stride, p.c.k_head_stride, p.c.k_key_stride, b, kvh, min(first + col, len - 1)), true, keys[kb]);
+    }
+    float acc[KB][16];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[kb][i] = 0.f;
+    const bool capped = p.cap2 != 0.f;
+    for (int s = 0; s < stages; ++s) {
+      Info these[TILES];
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) these[x] = next[x];
+      __builtin_amdgcn_s_waitcnt(0x0070);
+      __syncthreads();
+      if (s + 1 < stages) {
+        issue(s + 1);
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) next[x] = info((stages - 2 - s) * ROWS + (x * (NW / 2) + rw) * 32 + col);
+      }
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        const int pair0 = (stages - 1 - s) * ROWS + (x * (NW / 2) + rw) * 32;
+        if (pair0 < pairs) tile(lds + SHARE + (s & 1) * TILE + (x * (NW / 2) + rw) * 32 * S::ROWB, keys, these[x], pair0, my_key0, kw, capped, has_doc, acc);
+      }
+    }
+    // the rows' lanes together, then the waves that had the same keys
+    float *share = (float *)lds;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) acc[kb][i] += __shfl_xor(acc[kb][i], x);
+        if (col == 0) share[rw * KEYS + 32 * (KB * kw + kb) + S::key_of(i, hh)] = acc[kb][i];
+      }
+    __syncthreads();
+    if (adds) {
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW / 2; ++w) sum += share[w * KEYS + threadIdx.x];
+      out[mine] = before + sum;
+    }
+  }
+
+  // 32 rows meet this wave's keys
+  __device__ __forceinline__ void tile(const char *rows, const typename S::Rows (&keys)[KB], const Info &now, int pair0, int my_key0, int kw, bool capped, bool has_doc,
+                                       float (&acc)[KB][16]) const {
+    // rows that all see all of these keys, and whose scores need no more than a cap: the first row sees least
+    const int r0 = p.g_shift >= 0 ? pair0 >> p.g_shift : pair0 / p.G;
+    const int reach = min(max(len - n + from + r0, all - 1), len - 1);
+    const bool plain = !has_doc && !p.slopes && pair0 + 32 <= pairs && my_key0 + 32 * KB - 1 <= reach;
+    const float lse2 = is_none(now.lse) ? INFINITY : now.lse * kLog2e;  // a row that saw nothing gives nothing
+    f32x16_t a[KB];
+    products(rows, keys, a);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      bool raw = plain;
+      if (raw && capped) {
+        float far = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) far = fmaxf(fmaxf(far, fabsf(a[kb][i])), fabsf(a[kb][i + 1]));
+        raw = !__any(!(far <= p.cap_most));
+      }
+      if (raw) {
+        if (capped) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[kb][i] += exp2_(fmaf(a[kb][i], cap_factor(a[kb][i], p.cap_c), -lse2));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[kb][i] += exp2_(fmaf(a[kb][i], p.scale2, -lse2));
+        }
+      } else {
+        const int pair = pair0 + col, row = p.g_shift >= 0 ? pair >> p.g_shift : pair / p.G, own_index = len - n + from + row;
+        const int left = (pair < pairs ? min(max(own_index, all - 1), len - 1) : -1) - my_key0 - 32 * kb - 4 * hh;
+        const int pos = p.q_pos ? now.pos : p.c.prefix_len + own_index;
+        const int *ints = (const int *)lds + (NW / 2) * KEYS + 32 * (KB * kw + kb) + 4 * hh;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          i32x4_t doc = {-1, -1, -1, -1}, at = {0, 0, 0, 0};
+          if (has_doc) doc = *(const i32x4_t *)(ints + 8 * g);
+          if (p.slopes) at = *(const i32x4_t *)(ints + KEYS + 8 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * g + e;
+            float s = capped ? cap_any(a[kb][i], p.cap_c, p.cap_most, p.to_cap, p.cap2) : a[kb][i] * p.scale2;
+            if (p.slopes) s -= now.slope * kLog2e * fabsf((float)(pos - at[e]));
+            const bool seen = S::key_of(i, 0) <= left && (doc[e] == now.doc || doc[e] < 0 || now.doc < 0);
+            acc[kb][i] += seen ? exp2_(s - lse2) : 0.f;
+          }
+        }
+      }
+    }
+  }
+
+  // scores of 32 rows in LDS with this wave's keys: the operands of Span's products, exchanged
+  __device__ __forceinline__ void products(const char *rows, const typename S::Rows (&keys)[KB], f32x16_t (&a)[KB]) const {
+    constexpr int NP = S::NP, AHEAD = NP < 4 ? NP : 4;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) a[kb][r] = 0.f;
+    const unsigned row = here(S::lds_at(rows) + col * S::ROWB + ((hh ^ S::kswz(col)) << 4));
+    auto piece = [&](int i) { return *(const lds_f32x4_t *)(row ^ (i << 5)); };
+    f32x4_t q[NP];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) q[i] = piece(i);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        if constexpr (ES == 2) {
+          a[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, keys[kb].q[i]), __builtin_bit_cast(bf16x8_t, q[i]), a[kb], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) a[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].q[i][e], q[i][e], a[kb], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + AHEAD < NP) q[i + AHEAD] = piece(i + AHEAD);
+    }
+  }
+};
+
+template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> __global__ void __launch_bounds__(64 * NW, NW == 4 && NT <= 8 && sizeof(T) == 2 ? 3 : 2) k_span_received(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  using S = Span<T, NT, 4, 1, 32, WIDE>;
-  constexpr int ES = sizeof(T), EPC = 16 / ES;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hh = lane >> 5, col = lane & 31;
-  int id = blockIdx.x;
-  const int kvh = id % p.c.n_kv_heads;
-  id /= p.c.n_kv_heads;
-  const int b = id % p.c.n_requests, kb = id / p.c.n_requests;
-  const int len = uniform(span_len(p, b)), key0 = kb * kSpanReceivedKeys;
+  using R = Received<T, NT, WIDE, ROWS, KB, NW>;
+  const int blocks = (p.c.most + R::KEYS - 1) / R::KEYS, items = p.pairs_of_blocks ? (blocks + 1) / 2 : blocks;
+  int kvh, item;
+  if (!head_item(blockIdx.x, p.c.n_kv_heads, items * p.c.n_requests, kvh, item)) return;
+  const int b = item / items, i = item % items;
   const float *in = p.totals.in + b * p.totals.in_request_stride + kvh * p.totals.in_head_stride;
   float *out = p.totals.out + b * p.totals.out_request_stride + kvh * p.totals.out_head_stride;
-  const int64_t row0 = min(max((int64_t)p.q_start[b], (int64_t)0), p.n_rows), row1 = max(min((int64_t)p.q_start[b + 1], p.n_rows), row0);
-  const int n = (int)(row1 - row0);
-  int from = p.last > 0 ? max(0, n - p.last) : 0;               // the first row that counts
-  const int all = p.see_all ? clamped(p.see_all[b], 0, len) : 0;
-  if (key0 >= all) from = max(from, key0 - (len - n));          // rows before it see none of these keys
-  if (key0 >= len || from >= n) {
-    for (int j = key0 + threadIdx.x; j < min(p.c.most, key0 + kSpanReceivedKeys); j += 256) out[j] = in[j];
-    return;
+  R r(p, lds, kvh, b, uniform(span_len(p, b)));
+  if (!WIDE || r.span.chunks < R::S::CPR) {
+    const int end = p.one_stage ? R::LDS_ONE : R::LDS;
+    for (int x = threadIdx.x; x < end / 16; x += R::THREADS) ((f32x4_t *)lds)[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  S span(p, SpanKeys{0, 0, 0, len, b, kvh}, lds);
-  const int my_key0 = key0 + wave * 32;
-  // this wave's keys as the other operand: lane = key my_key0 + col
-  typename S::Rows keys;
-  {
-    const int key = min(my_key0 + col, len - 1);
-    span.load_row((const T *)p.c.k + own_offset(p.c, p.page_shift, p.c.k_page_stride, p.c.k_head_stride, p.c.k_key_stride, b, kvh, key), true, keys);
-  }
-  int key_doc[16], key_pos[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int key = min(my_key0 + S::key_of(i, hh), len - 1);
-    key_doc[i] = p.c.key_doc ? p.c.key_doc[b * p.c.key_doc_request_stride + kvh * p.c.key_doc_head_stride + key] : -1;
-    key_pos[i] = p.slopes ? (p.c.key_pos ? p.c.key_pos[b * p.c.key_pos_request_stride + kvh * p.c.key_pos_head_stride + key] : p.c.prefix_len + key) : 0;
-  }
-  const int pairs = (n - from) * p.G;
-  auto row_of = [&](int pair) { return row0 + from + pair / p.G; };
-  auto head_of = [&](int pair) { return kvh * p.G + pair % p.G; };
-  constexpr int TILE = 32 * S::ROWB;
-  if (!WIDE || span.chunks < S::CPR) {
-    for (int i = threadIdx.x; i < 2 * TILE / 16; i += 256) ((f32x4_t *)lds)[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    __syncthreads();
-  }
-  auto issue = [&](int tile, int buf) {
-    char *dst = lds + buf * TILE;
-    if constexpr (WIDE) {
-      constexpr int LOADS = (32 * S::CPR + 255) / 256;
-#pragma unroll
-      for (int j = 0; j < LOADS; ++j) {
-        const int at = (j * 4 + wave) * 64 + lane, row = at / S::CPR, c = (at % S::CPR) ^ S::kswz(row);
-        const int pair = min(tile * 32 + row, pairs - 1);
-        const char *src = (const char *)((const T *)p.q + row_of(pair) * p.q_rs + head_of(pair) * p.q_hs) + c * 16;
-        if (at < 32 * S::CPR && c < span.chunks) __builtin_amdgcn_global_load_lds((gbl_ptr_t *)src, (lds_ptr_t *)(dst + (j * 4 + wave) * 1024), 16, 0, 0);
-      }
-    } else {
-      const int d = p.c.head_dim;
-      for (int i = threadIdx.x; i < 32 * d; i += 256) {
-        const int row = i / d, f = i % d, c = (f / EPC) ^ S::kswz(row);
-        const int pair = min(tile * 32 + row, pairs - 1);
-        ((T *)(dst + row * S::ROWB + c * 16))[f % EPC] = ((const T *)p.q)[row_of(pair) * p.q_rs + head_of(pair) * p.q_hs + f];
-      }
-    }
-  };
-  struct Info { SpanRow r; float lse2; };
-  auto info = [&](int tile) {
-    const int pair = tile * 32 + col;
-    const bool there = pair < pairs;
-    const int64_t row = row_of(there ? pair : 0);
-    Info x;
-    x.r = span_row(p, (int)row, head_of(there ? pair : 0), b, len - n + (int)(row - row0), there);
-    const float lse = there ? p.lse_in[row_pair(p, x.r)] : -INFINITY;
-    x.lse2 = is_none(lse) ? INFINITY : lse * kLog2e;
-    return x;
-  };
-  float acc[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-  const int tiles = (pairs + 31) / 32;
-  issue(0, 0);
-  Info next = info(0);
-  for (int tile = 0; tile < tiles; ++tile) {
-    const Info now = next;
-    __builtin_amdgcn_s_waitcnt(0x0070);
-    __syncthreads();
-    if (tile + 1 < tiles) {
-      issue(tile + 1, (tile + 1) & 1);
-      next = info(tile + 1);
-    }
-    f32x16_t a;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) a[r] = 0.f;
-    const char *row = lds + (tile & 1) * TILE + col * S::ROWB;
-    const int x = S::kswz(col);
-#pragma unroll
-    for (int i = 0; i < S::NP; ++i) {
-      const f32x4_t q = *(const f32x4_t *)(row + (((2 * i + hh) ^ x) << 4));
-      if constexpr (ES == 2) {
-        a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, keys.q[i]), __builtin_bit_cast(bf16x8_t, q), a, 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) a = __builtin_amdgcn_mfma_f32_32x32x2f32(keys.q[i][e], q[e], a, 0, 0, 0);
-      }
-    }
-    float s[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = a[i];
-    if (p.cap2 != 0.f) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = cap_any(s[i], p.cap_c, p.cap_most, p.to_cap, p.cap2);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] *= p.scale2;
-    }
-    if (p.slopes) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] -= now.r.slope2 * fabsf((float)(now.r.pos - key_pos[i]));
-    }
-    const int last = min(now.r.lim, len - 1);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      bool seen = my_key0 + S::key_of(i, hh) <= last;
-      if (p.c.key_doc) seen = seen && (key_doc[i] == now.r.doc || key_doc[i] < 0 || now.r.doc < 0);
-      acc[i] += seen ? exp2_(s[i] - now.lse2) : 0.f;
-    }
-  }
-  // the rows' lanes together
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-#pragma unroll
-    for (int x = 1; x < 32; x <<= 1) acc[i] += __shfl_xor(acc[i], x);
-    const int key = my_key0 + S::key_of(i, hh);
-    if (col == 0 && key < p.c.most) out[key] = in[key] + acc[i];
-  }
+  r.block(i * R::KEYS, in, out);
+  if (p.pairs_of_blocks && blocks - 1 - i > i) r.block((blocks - 1 - i) * R::KEYS, in, out);
 }
 
 inline unsigned head_items(int heads, int items) { return 8u * ((unsigned)(heads >> 3) * items + ((unsigned)(heads & 7) * items + 7) / 8); }
@@ -391,8 +504,19 @@ template <typename T> hipError_t span_received(const SpanCall &p, bool wide, hip
   return span_pick(p.c.head_dim, wide, [&](auto nt, auto w) {
     constexpr int NT = decltype(nt)::value;
     constexpr bool W = decltype(w)::value;
-    const unsigned blocks = (unsigned)((p.c.most + kSpanReceivedKeys - 1) / kSpanReceivedKeys) * p.c.n_requests * p.c.n_kv_heads;
-    return span_launch<NT, W>(k_span_received<T, NT, W>, 2 * 32 * span_chunks(NT, sizeof(T)) * 16, blocks, 256, p, s);
+    constexpr int CPR = span_chunks(NT, sizeof(T));
+    SpanCall call = p;
+    auto go = [&](auto rows, auto kb, auto nw) {
+      constexpr int ROWS = decltype(rows)::value, KB = decltype(kb)::value, NW = decltype(nw)::value;
+      using R = Received<T, NT, W, ROWS, KB, NW>;
+      const int blocks = (p.c.most + R::KEYS - 1) / R::KEYS, items = p.pairs_of_blocks ? (blocks + 1) / 2 : blocks;
+      call.one_stage = p.last > 0 && (int64_t)p.last * p.G <= ROWS;
+      return span_launch<NT, W>(k_span_received<T, NT, W, ROWS, KB, NW>, call.one_stage ? R::LDS_ONE : R::LDS, head_items(p.c.n_kv_heads, items * p.c.n_requests), 64 * NW, call, s);
+    };
+    using std::integral_constant;
+    constexpr int few = CPR <= 32 ? 128 : 64;  // rows of a stage that fit LDS twice
+    if (!p.pairs_of_blocks) return go(integral_constant<int, few>(), integral_constant<int, 1>(), integral_constant<int, 4>());
+    return go(integral_constant<int, few>(), integral_constant<int, CPR <= 16 ? 2 : 1>(), integral_constant<int, few / 16>());
   });
 }
 

@@ -12,6 +12,7 @@ struct SpanCall {
   hyp_attn_cache_t c;
   int page_shift;             // log2(page_keys)
   int G, nq;
+  int g_shift;                // log2(G), -1: G is no power of two
   float scale2;               // scale * log2(e): scores are held as exponents of two
   float to_cap, cap2;         // scale / cap, cap * log2(e); cap2 0: not capped
   float cap_c[5], cap_most;   // polynomial of the capped score, and the largest raw score it is for
@@ -35,6 +36,8 @@ struct SpanCall {
   hyp_attn_totals_t totals;
   const float *lse_in;        // attn_received
   int last;
+  int pairs_of_blocks;        // a workgroup has a block of keys from the front and one from the back, or one block
+  int one_stage;              // the rows that count fit one stage
   int join_items;             // workgroups of the join that merge rows; the others add totals
 };
 
@@ -63,6 +66,5 @@ __host__ __device__ constexpr int span_token_waves(int nt, int es) { return span
 __host__ __device__ constexpr int span_steps_waves(int nt) { return nt <= 8 ? 2 : 1; }  // waves a SIMD that the registers are shared out for
 constexpr int kSpanWaves = 4;          // attn_prompt: waves of 32 rows
 constexpr int kSpanTile = 32 * kSpanWaves;
-constexpr int kSpanReceivedKeys = 128; // keys of a workgroup of attn_received
 
 }  // namespace hyp
