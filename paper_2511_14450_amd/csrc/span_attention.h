@@ -51,7 +51,7 @@ __device__ __forceinline__ bool head_item(int id, int heads, int items, int &hea
 // of `splits` parts of them.
 template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_prompt(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), WIDE>;
+  using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), 2, WIDE>;
   int kvh, item;
   if (!head_item(blockIdx.x, p.c.n_kv_heads, p.tiles * p.splits, kvh, item)) return;
   const int split = item % p.splits;
@@ -81,11 +81,11 @@ template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * 
 
 // attn_token.  Items over the shared keys, which all requests' rows meet at once, then items of up to 32 rows of one request
 // over its own keys, whose waves take turns at them.
-template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * span_token_waves(NT, sizeof(T))) k_span_token(const SpanCall p) {
+template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * span_token_waves(NT, sizeof(T)), span_steps_waves(NT)) k_span_token(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   constexpr int NW = span_token_waves(NT, sizeof(T));
-  using Own = Span<T, NT, 1, NW, 32, WIDE>;
-  using Pre = Span<T, NT, NW, 1, span_stage_keys(NT, sizeof(T)), WIDE>;
+  using Own = Span<T, NT, 1, NW, 32, 1, WIDE>;
+  using Pre = Span<T, NT, NW, 1, span_stage_keys(NT, sizeof(T)), 2, WIDE>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = threadIdx.x & 31;
   int id = blockIdx.x;
   const bool pre = id < p.pre_items;
@@ -130,77 +130,143 @@ template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * 
   span.join_waves(t, rows, (int64_t)b * p.G + tile * 32, p.pre_splits + split);
 }
 
-// The weight of a row's partial results: (maximum, sum) over the slots, in every lane.
-__device__ __forceinline__ float2 slots_total(const SpanCall &p, int slots, int64_t pair, int lane) {
+// (maximum, sum) of a row's partial results, in every lane; mine: the weight of the result in slot `lane`, where there is one, over 2^maximum
+__device__ __forceinline__ float2 slots_total(const SpanCall &p, int slots, int64_t pair, int lane, float &mine) {
   const int64_t all = p.n_rows * p.nq;
-  float m = -INFINITY;
-  for (int s = lane; s < slots; s += 64) m = fmaxf(m, p.part_ml[2 * (s * all + pair)]);
+  const float2 *ml = (const float2 *)p.part_ml;
+  const float2 first = lane < slots ? ml[lane * all + pair] : float2{-INFINITY, 0.f};
+  float m = first.x;
+  for (int s = lane + 64; s < slots; s += 64) m = fmaxf(m, ml[s * all + pair].x);
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-  float l = 0.f;
-  for (int s = lane; s < slots; s += 64) {
-    const float ms = p.part_ml[2 * (s * all + pair)];
-    if (!is_none(ms)) l += exp2_(ms - m) * p.part_ml[2 * (s * all + pair) + 1];
+  mine = is_none(first.x) ? 0.f : exp2_(first.x - m) * first.y;
+  float l = mine;
+  for (int s = lane + 64; s < slots; s += 64) {
+    const float2 x = ml[s * all + pair];
+    if (!is_none(x.x)) l += exp2_(x.x - m) * x.y;
   }
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
   return {m, l};
 }
 
-// Partial results to results, a wave a row; then, for attn_token, the weight that own keys got.
+// Partial results to results, a wave a row, V features a lane; all of a row's partial results are requested before the first is waited for.
+template <typename T, int V> __device__ __forceinline__ void join_row(const SpanCall &p, int slots, int64_t pair, int lane) {
+  const int d = p.c.head_dim, f = lane * V;
+  const int64_t all = p.n_rows * p.nq, row = pair / p.nq;
+  const int head = (int)(pair - row * p.nq);
+  if (p.q_start && (row < p.q_start[0] || row >= p.q_start[p.c.n_requests])) return;  // no request's row
+  float weight;
+  const float2 ml = slots_total(p, slots, pair, lane, weight);
+  const bool none = is_none(ml.x);
+  if (p.lse && lane == 0) p.lse[pair] = none ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2;
+  const float inv = none ? 0.f : 1.0f / ml.y;
+  float acc[V] = {};
+  const bool on = f < d;  // V divides d
+  for (int s0 = 0; s0 < slots; s0 += 8) {
+    float o[8][V], w[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int s = s0 + u;
+      w[u] = 0.f;
+      if (s < slots) {
+        if (s < 64) w[u] = __shfl(weight, s);
+        else {
+          const float2 x = ((const float2 *)p.part_ml)[s * all + pair];
+          w[u] = is_none(x.x) ? 0.f : exp2_(x.x - ml.x) * x.y;
+        }
+        const float *src = p.part_o + (s * all + pair) * d + f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[u][e] = on ? src[e] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (!is_zero(w[u])) {  // an empty slot holds nothing, not even zeros
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = fmaf(w[u] * inv, o[u][e], acc[e]);
+      }
+  }
+  if (!on) return;
+  T *out = (T *)p.out + row * p.out_rs + head * p.out_hs + f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) store_f32(out + e, acc[e]);
+}
+
+// The same for head sizes that neither two nor four features a lane fit.
+template <typename T> __device__ __forceinline__ void join_odd(const SpanCall &p, int slots, int64_t pair, int lane) {
+  const int d = p.c.head_dim;
+  const int64_t all = p.n_rows * p.nq, row = pair / p.nq;
+  const int head = (int)(pair - row * p.nq);
+  if (p.q_start && (row < p.q_start[0] || row >= p.q_start[p.c.n_requests])) return;
+  float weight;
+  const float2 ml = slots_total(p, slots, pair, lane, weight);
+  const bool none = is_none(ml.x);
+  if (p.lse && lane == 0) p.lse[pair] = none ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2;
+  for (int f = lane; f < d; f += 64) {
+    float acc = 0.f;
+    for (int s = 0; s < slots; ++s) {
+      const float2 x = ((const float2 *)p.part_ml)[s * all + pair];
+      if (!is_none(x.x)) acc = fmaf(exp2_(x.x - ml.x) * x.y / ml.y, p.part_o[(s * all + pair) * d + f], acc);
+    }
+    store_f32((T *)p.out + row * p.out_rs + head * p.out_hs + f, acc);
+  }
+}
+
+// ... and for attn_token the weight that own keys got, 1024 of one request and KV head to a workgroup.
 template <typename T> __global__ void __launch_bounds__(256) k_span_join(const SpanCall p, int slots) {
   __shared__ float lse2[256];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = p.c.head_dim;
-  const int64_t all = p.n_rows * p.nq;
   if ((int)blockIdx.x < p.join_items) {
     const int64_t pair = (int64_t)blockIdx.x * 4 + wave;
-    if (pair >= all) return;
-    const int64_t row = pair / p.nq;
-    if (p.q_start && (row < p.q_start[0] || row >= p.q_start[p.c.n_requests])) return;  // no request's row
-    const float2 ml = slots_total(p, slots, pair, lane);
-    const int head = (int)(pair - row * p.nq);
-    T *out = (T *)p.out + row * p.out_rs + head * p.out_hs;
-    const bool none = is_none(ml.x);
-    if (p.lse && lane == 0) p.lse[pair] = none ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2;
-    const float inv = none ? 0.f : 1.0f / ml.y;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < slots; ++s) {
-      const float ms = p.part_ml[2 * (s * all + pair)];
-      if (is_none(ms)) continue;
-      const float a = exp2_(ms - ml.x) * p.part_ml[2 * (s * all + pair) + 1] * inv;
-      const float *o = p.part_o + (s * all + pair) * d;
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        if (lane + 64 * x < d) acc[x] = fmaf(a, o[lane + 64 * x], acc[x]);
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (lane + 64 * x < d) store_f32(out + lane + 64 * x, acc[x]);
+    if (pair >= p.n_rows * p.nq) return;
+    if (d <= 64) join_row<T, 1>(p, slots, pair, lane);
+    else if (d <= 128 && (d & 1) == 0) join_row<T, 2>(p, slots, pair, lane);
+    else if ((d & 3) == 0) join_row<T, 4>(p, slots, pair, lane);
+    else join_odd<T>(p, slots, pair, lane);
     return;
   }
-  // 1024 keys of one request and KV head
   const int blocks = (p.c.most + 1023) / 1024;
   int id = blockIdx.x - p.join_items;
   const int kb = id % blocks;
   id /= blocks;
   const int kvh = id % p.c.n_kv_heads, b = id / p.c.n_kv_heads;
-  const int len = uniform(span_len(p, b));
+  const int len = uniform(span_len(p, b)), j = kb * 1024 + threadIdx.x * 4;
   const float *in = p.totals.in + b * p.totals.in_request_stride + kvh * p.totals.in_head_stride;
   float *out = p.totals.out + b * p.totals.out_request_stride + kvh * p.totals.out_head_stride;
+  float sum[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum[e] = j + e < p.c.most ? in[j + e] : 0.f;
   if (kb * 1024 < len) {
     for (int g = wave; g < p.G; g += 4) {
-      const float2 ml = slots_total(p, slots, (int64_t)b * p.nq + kvh * p.G + g, lane);
+      float weight;
+      const float2 ml = slots_total(p, slots, (int64_t)b * p.nq + kvh * p.G + g, lane, weight);
       if (lane == 0) lse2[g] = is_none(ml.x) ? INFINITY : ml.x + __builtin_amdgcn_logf(ml.y);
     }
   }
   __syncthreads();
-  const float *scores = p.scores + ((int64_t)b * p.c.n_kv_heads + kvh) * p.G * p.score_pitch;
-  for (int j = kb * 1024 + threadIdx.x; j < min(p.c.most, kb * 1024 + 1024); j += 256) {
-    float w = 0.f;
-    if (j < len)
-      for (int g = 0; g < p.G; ++g) w += exp2_(scores[g * p.score_pitch + j] - lse2[g]);
-    out[j] = in[j] + w;
+  const float *scores = p.scores + ((int64_t)b * p.c.n_kv_heads + kvh) * p.G * p.score_pitch + j;
+  if (j < len) {
+    f32x4_t w = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = 0; g0 < p.G; g0 += 4) {
+      f32x4_t s[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (g0 + u < p.G) s[u] = *(const f32x4_t *)(scores + (g0 + u) * p.score_pitch);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (g0 + u < p.G) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] += exp2_(s[u][e] - lse2[g0 + u]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < len) sum[e] += w[e];
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e < p.c.most) out[j + e] = sum[e];
 }
 
 // attn_received.  A workgroup: a block of own keys of a request and KV head, 64 KB of them, or one from the front and one from the back, so
@@ -209,7 +275,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_span_join(const S
 // at about the same time.  What a key gets is summed in its lane over the rows, then over lanes and waves, in a fixed order.
 // Rows come from L2 for every block of keys: 64 keys of 128 bf16 features to a block made that the bound (4.5 TB/s).
 template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> struct Received {
-  using S = Span<T, NT, NW, 1, 32, WIDE>;
+  using S = Span<T, NT, NW, 1, 32, 1, WIDE>;
   static constexpr int ES = sizeof(T), EPC = 16 / ES, KEYS = 64 * KB, THREADS = 64 * NW, TILE = ROWS * S::ROWB;
   static constexpr int SHARE = ((NW / 2) * KEYS * 4 + 2 * KEYS * 4 + 1023) / 1024 * 1024, LDS_ONE = SHARE + TILE, LDS = LDS_ONE + TILE;
   static constexpr int LOADS = ROWS * S::CPR / THREADS, STEP = THREADS / S::CPR;  // a lane's loads of a stage, and the rows between them
@@ -482,7 +548,7 @@ template <typename T> hipError_t span_prompt(const SpanCall &p, bool wide, hipSt
   return span_pick(p.c.head_dim, wide, [&](auto nt, auto w) {
     constexpr int NT = decltype(nt)::value;
     constexpr bool W = decltype(w)::value;
-    using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), W>;
+    using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), 2, W>;
     const int lds = S::LDS_ALL + (p.c.key_doc ? Survey<S>::LDS : 0);
     return span_launch<NT, W>(k_span_prompt<T, NT, W>, lds,
                               head_items(p.c.n_kv_heads, p.tiles * p.splits), 64 * kSpanWaves, p, s);
@@ -494,7 +560,7 @@ template <typename T> hipError_t span_token(const SpanCall &p, bool wide, hipStr
     constexpr int NT = decltype(nt)::value;
     constexpr bool W = decltype(w)::value;
     constexpr int NW = span_token_waves(NT, sizeof(T));
-    constexpr int own = Span<T, NT, 1, NW, 32, W>::LDS_ALL, pre = Span<T, NT, NW, 1, span_stage_keys(NT, sizeof(T)), W>::LDS_ALL;
+    constexpr int own = Span<T, NT, 1, NW, 32, 1, W>::LDS_ALL, pre = Span<T, NT, NW, 1, span_stage_keys(NT, sizeof(T)), 2, W>::LDS_ALL;
     return span_launch<NT, W>(k_span_token<T, NT, W>, own > pre ? own : pre,
                               (unsigned)p.pre_items + (unsigned)p.c.n_requests * p.tiles * p.splits * p.c.n_kv_heads, 64 * NW, p, s);
   });

@@ -127,8 +127,9 @@ __device__ inline int64_t pair_at(const SpanCall &p, int64_t first, int kvh, int
   return row * p.nq + kvh * p.G + (x - row * p.G);
 }
 
-// RW waves of 32 rows each, KW waves that take turns at the keys; SKW keys of a wave in a stage.
-template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
+// RW waves of 32 rows each, KW waves that take turns at the keys; SKW keys of a wave in a stage; NBUF stages in LDS: with one, another
+// workgroup of the CU computes while this one loads.
+template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> struct Span {
   static constexpr int ES = sizeof(T), NW = RW * KW, THREADS = 64 * NW;
   static constexpr int CPR = span_chunks(NT, ES), ROWB = CPR * 16;  // an LDS row
   static constexpr int EPC = 16 / ES;                               // elements of a piece
@@ -136,8 +137,8 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
   static constexpr int NDB = NT / 2;                                // 32-feature blocks of the output
   static constexpr int SKEYS = KW * SKW, NKB = SKW / 32;
   static constexpr int TILE = SKEYS * ROWB, BUF = 2 * TILE;         // keys, then values
-  static constexpr int INTS = 2 * BUF;                              // ids and positions of the stages' keys, after two buffers
-  static constexpr int LDS = INTS + 2 * 2 * SKEYS * 4;
+  static constexpr int INTS = NBUF * BUF;                           // ids and positions of the stages' keys, after the buffers
+  static constexpr int LDS = INTS + NBUF * 2 * SKEYS * 4;
   static constexpr int JOIN = KW > 1 ? KW * (NDB * 32 * 33 + 64) * 4 : 0;
   static constexpr int LDS_ALL = LDS > JOIN ? LDS : JOIN;
   static_assert(LDS_ALL <= 160 * 1024, "LDS of a CU");
@@ -194,7 +195,7 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
   // Pieces of a row behind the features count as zero in every product; they are never written after this.
   __device__ __forceinline__ void clear_padding() {
     if (!WIDE || chunks < CPR) {
-      for (int i = threadIdx.x; i < 2 * BUF / 16; i += THREADS) ((f32x4_t *)lds)[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int i = threadIdx.x; i < NBUF * BUF / 16; i += THREADS) ((f32x4_t *)lds)[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       __syncthreads();
     }
   }
@@ -614,9 +615,13 @@ template <typename T, int NT, int RW, int KW, int SKW, bool WIDE> struct Span {
       const int then = way.next(st + 1, st1);
       __builtin_amdgcn_s_waitcnt(0x0070);  // this wave's share of the stage has landed
       __syncthreads();                     // all shares have, and the other buffer is free
-      if (then < st1) issue(then, buf ^ 1);
+      if (NBUF > 1 && then < st1) issue(then, buf ^ 1);
       compute(stage_of(st), buf, rows, r, lim_lo, lim_hi, way.hides(st), t, score_out);
-      buf ^= 1;
+      if constexpr (NBUF > 1) buf ^= 1;
+      else if (then < st1) {
+        __syncthreads();
+        issue(then, 0);
+      }
       st = then;
     }
     t.l = half_sum(t.l);

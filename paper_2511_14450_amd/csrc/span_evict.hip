@@ -17,29 +17,15 @@ __device__ __forceinline__ int64_t key_offset(const hyp_attn_cache_t &c, int shi
   return (int64_t)page * page_stride + (int64_t)kvh * head_stride + (int64_t)(j & (c.page_keys - 1)) * key_stride;
 }
 
-// Exclusive count of `flag` over the workgroup's threads before this one; total: over all.  Two barriers.
-__device__ __forceinline__ int count_before(bool flag, int *waves, int &total) {
-  const unsigned long long votes = __ballot(flag);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane == 0) waves[wave] = __popcll(votes);
-  __syncthreads();
-  int before = 0, sum = 0;
-#pragma unroll
-  for (int w = 0; w < kSelectThreads / 64; ++w) {
-    const int n = waves[w];
-    before += w < wave ? n : 0;
-    sum += n;
-  }
-  __syncthreads();
-  total = sum;
-  return before + __popcll(votes & ((1ull << lane) - 1));
-}
-
-// One request and KV head.  The keep-th largest total is found by four counts of eight bits each; then one pass in the order of
-// the slots says who stays (of equal totals the lowest slots), which slots become free and which keys move there.
+// One request and KV head.  The keep-th largest total is found by three counts of 11, 11 and 10 bits; then one look at the totals in the
+// order of the slots says who stays (of equal totals the lowest slots), which slots become free and which keys move there.  A thread has
+// eight keys of each 8192, 1024 apart: up to so many keys are read once and stay in registers, more are read for every look.  Latency
+// bounds it, of the one read and of about twenty barriers; 64 caches of 8192 keys took 27 us with a read for each of four counts and barriers for
+// every 1024 keys.
+constexpr int kItems = 8, kBlock = kSelectThreads * kItems, kWaves = kSelectThreads / 64;
 __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall p) {
-  __shared__ int hist[256], waves[kSelectThreads / 64], found[2];
-  const int b = blockIdx.x / p.c.n_kv_heads, kvh = blockIdx.x % p.c.n_kv_heads, tid = threadIdx.x, K = p.keep;
+  __shared__ int hist[2048], before[kItems * kWaves], before2[kItems * kWaves], found[2], wave_sum[kWaves];
+  const int b = blockIdx.x / p.c.n_kv_heads, kvh = blockIdx.x % p.c.n_kv_heads, tid = threadIdx.x, K = p.keep, lane = tid & 63, wave = tid >> 6;
   const int len = clamped(p.c.lens[b], 0, p.c.most);
   int *kept = p.kept + (int64_t)blockIdx.x * K;
   if (len <= K) {
@@ -51,72 +37,124 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
   const int64_t first = (int64_t)p.c.prefix_len + p.sink;
   const int64_t newest = (p.now ? (int64_t)p.now[b] : (int64_t)p.c.prefix_len + len) - p.recent;
   // order of the keys as unsigned numbers: a NaN lowest, -0 as 0, what is always kept highest
-  auto rank = [&](int j) -> unsigned {
-    const int64_t at = pos ? (int64_t)pos[j] : (int64_t)p.c.prefix_len + j;
-    if (at < first || at >= newest) return 0xffffffffu;
-    const unsigned u = __float_as_uint(totals[j]);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
-    if ((u & 0x7fffffffu) == 0u) return 0x80000000u;
-    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+  unsigned u[kItems];
+  auto read = [&](int block) {
+    float t[kItems];
+    int at[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int j = min(block + i * kSelectThreads + tid, len - 1);
+      t[i] = totals[j];
+      at[i] = pos ? pos[j] : p.c.prefix_len + j;
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const unsigned x = __float_as_uint(t[i]);
+      u[i] = at[i] < first || at[i] >= newest ? 0xffffffffu
+             : (x & 0x7fffffffu) > 0x7f800000u ? 0u
+             : (x & 0x7fffffffu) == 0u ? 0x80000000u : x ^ ((x >> 31) ? 0xffffffffu : 0x80000000u);
+    }
   };
+  const bool once = len <= kBlock;
+  if (once) read(0);
   unsigned prefix = 0, mask = 0;
   int need = K;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+  for (int look = 0; look < 3; ++look) {
+    const int shift = look == 0 ? 21 : look == 1 ? 10 : 0, bins = look == 2 ? 1024 : 2048;
+    hist[tid] = hist[tid + 1024] = 0;
     __syncthreads();
-    for (int j = tid; j < len; j += kSelectThreads) {
-      const unsigned u = rank(j);
-      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255], 1);
+    for (int block = 0; block < len; block += kBlock) {
+      if (!once) read(block);
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+        if (block + i * kSelectThreads + tid < len && (u[i] & mask) == prefix) atomicAdd(&hist[(u[i] >> shift) & (bins - 1)], 1);
     }
     __syncthreads();
-    if (tid < 64) {  // bins 4 lane .. 4 lane + 3, counted from the highest
-      int own[4], sum = 0;
+    // two bins a thread, counted from the highest; the bin in which the need is met
+    const int hi = bins - 1 - 2 * tid, own0 = hi > 0 ? hist[hi] : 0, own1 = hi > 0 ? hist[hi - 1] : 0;
+    int upto = own0 + own1;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sum += own[x] = hist[255 - (4 * tid + x)];
-      int upto = sum;
+    for (int s = 1; s < 64; s <<= 1) {
+      const int v = __shfl_up(upto, s);
+      if (lane >= s) upto += v;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    int above = upto - own0 - own1;
 #pragma unroll
-      for (int s = 1; s < 64; s <<= 1) {
-        const int v = __shfl_up(upto, s);
-        if (tid >= s) upto += v;
-      }
-      int above = upto - sum;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (above < need && need <= above + own[x]) {
-          found[0] = 255 - (4 * tid + x);
-          found[1] = need - above;
-        }
-        above += own[x];
-      }
+    for (int w = 0; w < kWaves; ++w) above += w < wave ? wave_sum[w] : 0;
+    if (above < need && need <= above + own0) {
+      found[0] = hi;
+      found[1] = need - above;
+    } else if (above + own0 < need && need <= above + own0 + own1) {
+      found[0] = hi - 1;
+      found[1] = need - above - own0;
     }
     __syncthreads();
     prefix |= (unsigned)found[0] << shift;
-    mask |= 255u << shift;
+    mask |= (unsigned)(bins - 1) << shift;
     need = found[1];
-    __syncthreads();
   }
   int *holes = p.list + (int64_t)blockIdx.x * 2 * K, *moved = holes + K;
+  const unsigned long long below = (1ull << lane) - 1;
+  // votes of eight flags to the count of all flags of lower slots in this block; base: of the blocks before, moved on
+  auto count = [&](const unsigned long long (&votes)[kItems], int *where, int &base, int (&out)[kItems]) {
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) where[i * kWaves + wave] = __popcll(votes[i]);
+    }
+    __syncthreads();
+    if (wave == 0) {  // 128 counts, two a lane
+      const int x = where[2 * lane], y = where[2 * lane + 1];
+      int upto = x + y;
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) {
+        const int v = __shfl_up(upto, s);
+        if (lane >= s) upto += v;
+      }
+      where[2 * lane] = upto - x - y;
+      where[2 * lane + 1] = upto - y;
+      if (lane == 63) found[0] = upto;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) out[i] = base + where[i * kWaves + wave] + __popcll(votes[i] & below);
+    base += found[0];
+  };
   int equal = 0, n_holes = 0, n_moved = 0;
-  for (int j0 = 0; j0 < len; j0 += kSelectThreads) {
-    const int j = j0 + tid;
-    const unsigned u = j < len ? rank(j) : 0u;
-    const bool same = j < len && u == prefix;
-    int n;
-    const int nth = equal + count_before(same, waves, n);
-    equal += n;
-    const bool stays = j < len && (u > prefix || (same && nth < need));
-    const bool hole = j < K && !stays, mover = j >= K && stays;
-    if (j0 < K) {
-      const int at = n_holes + count_before(hole, waves, n);
-      n_holes += n;
-      if (hole) holes[at] = j;
-      else if (j < K) kept[j] = j;
+  for (int block = 0; block < len; block += kBlock) {
+    if (!once) read(block);
+    unsigned long long votes[kItems], hole_votes[kItems], move_votes[kItems];
+    int nth[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) votes[i] = __ballot(block + i * kSelectThreads + tid < len && u[i] == prefix);
+    count(votes, before, equal, nth);
+    unsigned stays = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int j = block + i * kSelectThreads + tid;
+      const bool s = j < len && (u[i] > prefix || (u[i] == prefix && nth[i] < need));
+      stays |= (unsigned)s << i;
+      hole_votes[i] = __ballot(j < K && !s);
+      move_votes[i] = __ballot(j >= K && s);
     }
-    if (j0 + kSelectThreads > K) {
-      const int at = n_moved + count_before(mover, waves, n);
-      n_moved += n;
-      if (mover) moved[at] = j;
+    int hole_at[kItems], move_at[kItems];
+    __syncthreads();
+    count(hole_votes, before2, n_holes, hole_at);
+    __syncthreads();
+    count(move_votes, before, n_moved, move_at);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int j = block + i * kSelectThreads + tid;
+      const bool s = (stays >> i) & 1;
+      if (j < K) {
+        if (s) kept[j] = j;
+        else holes[hole_at[i]] = j;
+      } else if (s) {
+        moved[move_at[i]] = j;
+      }
     }
+    __syncthreads();
   }
   __threadfence_block();
   __syncthreads();
@@ -129,6 +167,8 @@ template <bool VEC, int ES> __global__ void __launch_bounds__(256) k_evict_move(
   const int pair = blockIdx.x / per, r0 = (blockIdx.x % per) * kMoveRows;
   const int b = pair / p.c.n_kv_heads, kvh = pair % p.c.n_kv_heads, d = p.c.head_dim, rows = min(kMoveRows, p.keep - r0);
   const int *kept = p.kept + (int64_t)pair * p.keep + r0;
+  // the kernel before was the last to read the old length
+  if (kvh == 0 && r0 == 0 && threadIdx.x == 0) p.to.lens[b] = min(clamped(p.c.lens[b], 0, p.c.most), p.keep);
   if (threadIdx.x < rows) {
     const int r = r0 + threadIdx.x, src = kept[threadIdx.x];
     if (src >= 0 && !(p.in_place && src == r)) {
@@ -159,12 +199,6 @@ template <bool VEC, int ES> __global__ void __launch_bounds__(256) k_evict_move(
   }
 }
 
-// after every reader of the old lengths
-__global__ void k_evict_lens(const int *lens, int *to, int n, int most, int keep) {
-  const int b = blockIdx.x * blockDim.x + threadIdx.x;
-  if (b < n) to[b] = min(clamped(lens[b], 0, most), keep);
-}
-
 }  // namespace
 
 hipError_t span_evict(const EvictCall &p, hipStream_t s) {
@@ -178,7 +212,6 @@ hipError_t span_evict(const EvictCall &p, hipStream_t s) {
     if (p.vec) k_evict_move<true, 4><<<blocks, 256, 0, s>>>(p);
     else k_evict_move<false, 4><<<blocks, 256, 0, s>>>(p);
   }
-  k_evict_lens<<<(p.c.n_requests + 255) / 256, 256, 0, s>>>(p.c.lens, p.to.lens, p.c.n_requests, p.c.most, p.keep);
   return hipGetLastError();
 }
 

@@ -7,10 +7,10 @@
 namespace hyp {
 
 // attn_prompt: parts that the keys of a row tile are cut into.  Without a cut a tile's workgroup meets all its keys; that fills the
-// chip from one workgroup a CU on.
-inline int span_prompt_splits(int64_t workgroups, int64_t stages) {
-  if (workgroups >= 256 || stages < 8) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(workgroups, 1), stages / 4, 64}));
+// chip from one workgroup a CU on.  fewest: stages of a part, below which joining costs more than it gains.
+inline int span_prompt_splits(int64_t workgroups, int64_t stages, int64_t fewest) {
+  if (workgroups >= 256 || stages < 2 * fewest) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(workgroups, 1), stages / fewest, 64}));
 }
 
 struct SpanTokenPlan { int pre_wide, pre_tiles, pre_splits, tiles, splits; };
