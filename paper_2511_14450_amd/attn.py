@@ -187,12 +187,25 @@ def _totals(cache: AttnCache, totals: torch.Tensor, totals_out: Optional[torch.T
     return _Totals(totals.data_ptr(), out.data_ptr(), totals.stride(0), totals.stride(1), out.stride(0), out.stride(1))
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream):
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
-def _handle(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _handle(stream, device: torch.device) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(device.index)
+
+
+def _slow_raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the handle alone, without the Stream object around it, which takes a third of a small call's time
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _slow_raw_stream)
 
 
 def _outputs(cache: AttnCache, q: torch.Tensor, out, lse):
@@ -232,7 +245,7 @@ def attn_prompt(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: torc
         out, lse, o = _outputs(cache, q, out, lse)
         need = lib.attn_workspace_bytes(cache._ref, C.byref(rows), None) if workspace is None else 0
         workspace, ptr, size = _workspace(need, workspace, q.device)
-        _check(lib.attn_prompt(cache._ref, rule._ref, C.byref(rows), C.byref(o), ptr, size, _handle(stream)))
+        _check(lib.attn_prompt(cache._ref, rule._ref, C.byref(rows), C.byref(o), ptr, size, _handle(stream, cache.device)))
     return out, lse
 
 
@@ -248,7 +261,7 @@ def attn_token(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_pos: Optiona
         t = None if totals is None else C.byref(_totals(cache, totals, totals_out, cache.most))
         need = lib.attn_workspace_bytes(cache._ref, C.byref(rows), t) if workspace is None else 0
         workspace, ptr, size = _workspace(need, workspace, q.device)
-        _check(lib.attn_token(cache._ref, rule._ref, C.byref(rows), C.byref(o), t, ptr, size, _handle(stream)))
+        _check(lib.attn_token(cache._ref, rule._ref, C.byref(rows), C.byref(o), t, ptr, size, _handle(stream, cache.device)))
     return out, lse
 
 
@@ -260,7 +273,7 @@ def attn_received(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: to
     if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous():
         raise ValueError("lse: need a contiguous float32 device tensor [rows, query heads]")
     t = _totals(cache, totals, totals_out, cache.most)
-    _check(_lib().attn_received(cache._ref, rule._ref, C.byref(rows), lse.data_ptr(), last, C.byref(t), _handle(stream)))
+    _check(_lib().attn_received(cache._ref, rule._ref, C.byref(rows), lse.data_ptr(), last, C.byref(t), _handle(stream, cache.device)))
     return totals if totals_out is None else totals_out
 
 
@@ -279,5 +292,5 @@ def attn_evict(cache: AttnCache, totals: torch.Tensor, keep: int, sink: int = 0,
         workspace, ptr, size = _workspace(need, workspace, cache.device)
         _check(lib.attn_evict(cache._ref, None if into is None else into._ref, C.byref(t), keep, sink, recent,
                               None if now is None else _ints(now, (cache.n_requests,), "now"),
-                              _ints(kept, (cache.n_requests, cache.n_kv_heads, max(keep, 0)), "kept"), ptr, size, _handle(stream)))
+                              _ints(kept, (cache.n_requests, cache.n_kv_heads, max(keep, 0)), "kept"), ptr, size, _handle(stream, cache.device)))
     return kept

@@ -141,15 +141,17 @@ struct Plan {
 };
 
 Plan plan_prompt(SpanCall &p, bool wide) {
-  const int es = es_of(p.c), stage = span_stage_keys(span_steps(p.c.head_dim, wide), es);
-  const int64_t tiles = p.n_rows * p.G / kSpanTile + p.c.n_requests;
+  const int es = es_of(p.c), nt = span_steps(p.c.head_dim, wide);
+  const int64_t pairs = p.n_rows * p.G;
+  const int64_t stage = span_stage_keys(nt, es);
+  const int64_t tiles = pairs / kSpanTile + p.c.n_requests;
   const int64_t stages = (p.c.prefix_len + stage - 1) / stage + (p.c.most + stage - 1) / stage;
   p.tiles = (int)tiles;
   p.splits = span_prompt_splits(tiles * p.c.n_kv_heads, stages, es == 2 ? 4 : 2);
   need(tiles * p.splits * (p.c.n_kv_heads + 8) < (1ll << 31), HYP_ESHAPE, "too many row tiles for a launch");
   Plan w;
   if (p.splits > 1) {
-    w.part_o = ((int64_t)p.splits * p.n_rows * p.nq * p.c.head_dim + 3) / 4 * 4;  // pairs of floats follow
+    w.part_o = (p.splits * p.n_rows * p.nq * p.c.head_dim + 3) / 4 * 4;  // pairs of floats follow
     w.part_ml = (int64_t)p.splits * p.n_rows * p.nq * 2;
   }
   return w;

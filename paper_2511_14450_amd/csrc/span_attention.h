@@ -2,28 +2,39 @@
 // translation unit per type.
 #pragma once
 
+#include <atomic>
+#include <type_traits>
+
 #include "span_core.h"
 #include "span_survey.h"
 
 namespace hyp {
 namespace {
 
-// The request of row tile `t`: request b's tiles start at floor(q_start[b] G / tile) + b, which leaves each as many as it
-// needs, or one more.  Returns the tile's first pair inside the request, or -1 if there is none.
-__device__ __forceinline__ int64_t tile_request(const SpanCall &p, int t, int tile, int &req, int64_t &row0, int &rows) {
-  const int n = p.c.n_requests;
-  auto start = [&](int b) { return min(max((int64_t)p.q_start[b], (int64_t)0), p.n_rows); };
-  int lo = 0, hi = n - 1;  // the last request whose first tile is <= t
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (start(mid) * p.G / tile + mid <= t) lo = mid;
-    else hi = mid - 1;
-  }
-  req = uniform(lo);
-  row0 = uniform((int)start(req));
-  rows = uniform((int)max(start(req + 1) - row0, (int64_t)0));
-  const int64_t first = ((int64_t)t - (row0 * p.G / tile + req)) * tile;
-  return first >= 0 && first < (int64_t)rows * p.G ? first : -1;
+// The request of a row tile, its rows and its own keys.
+struct TileRequest { int req, row0, rows, len, see_all; int64_t first; };  // first: the tile's first pair inside the request, -1: none
+
+// Request b's tiles start at floor(q_start[b] G / tile) + b, which leaves each as many as it needs, or one more.  The lanes look at 64
+// requests each, all that is to be known of them requested at once: one after the other these loads were a third of a small call's time.
+__device__ __forceinline__ TileRequest tile_request(const SpanCall &p, int t, int tile) {
+  const int n = p.c.n_requests, lane = threadIdx.x & 63;
+  auto cut = [&](int v) { return (int)min(max((int64_t)v, (int64_t)0), p.n_rows); };
+  auto first_tile = [&](int row, int b) { return (int64_t)row * p.G / tile + b; };
+  int base = 0;
+  while (base + 64 < n && first_tile(uniform(cut(p.q_start[base + 64])), base + 64) <= t) base += 64;
+  const int b = min(base + lane, n - 1);
+  const int from = cut(p.q_start[b]), to = cut(p.q_start[b + 1]), len = span_len(p, b), all = p.see_all ? p.see_all[b] : 0;
+  const unsigned long long votes = __ballot(first_tile(from, b) <= t);
+  const int who = max(63 - __builtin_clzll(votes | 1), 0);
+  TileRequest x;
+  x.req = min(base + who, n - 1);
+  x.row0 = __builtin_amdgcn_readlane(from, who);
+  x.rows = max(__builtin_amdgcn_readlane(to, who) - x.row0, 0);
+  x.len = __builtin_amdgcn_readlane(len, who);
+  x.see_all = __builtin_amdgcn_readlane(all, who);
+  const int64_t first = ((int64_t)t - first_tile(x.row0, x.req)) * tile;
+  x.first = first >= 0 && first < (int64_t)x.rows * p.G ? first : -1;
+  return x;
 }
 
 // Which head and item a workgroup has.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: whole heads to one XCD
@@ -47,35 +58,29 @@ __device__ __forceinline__ bool head_item(int id, int heads, int items, int &hea
   return item < items;
 }
 
-// attn_prompt.  A workgroup: one KV head, 128 rows of one request (dense over the group's heads), all the keys they see or one
-// of `splits` parts of them.
-template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_prompt(const SpanCall p) {
+// attn_prompt.  A workgroup: one KV head, rows of one request (dense over the group's heads), all the keys they see or one of `splits` parts
+// of them: 128 rows, 32 a wave, whose waves meet the same keys.
+template <typename T, int NT, bool WIDE>
+__global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_prompt(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), 2, WIDE>;
   int kvh, item;
   if (!head_item(blockIdx.x, p.c.n_kv_heads, p.tiles * p.splits, kvh, item)) return;
-  const int split = item % p.splits;
-  const int tile = p.tiles - 1 - item / p.splits;  // the longest rows of a request first
-  int req, n;
-  int64_t row0;
-  const int64_t first = tile_request(p, tile, kSpanTile, req, row0, n);
-  if (first < 0) return;
+  const int split = p.splits > 1 ? item % p.splits : 0;
+  const TileRequest q = tile_request(p, p.tiles - 1 - (p.splits > 1 ? item / p.splits : item), kSpanTile);  // the longest rows of a request first
+  if (q.first < 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = threadIdx.x & 31;
-  const int len = uniform(span_len(p, req));
-  const int64_t pair = first + wave * 32 + col;
-  const bool there = pair < (int64_t)n * p.G;
-  const int i = there ? (int)(pair / p.G) : 0, g = there ? (int)(pair - (int64_t)i * p.G) : 0;
-  const SpanRow r = span_row(p, (int)row0 + i, kvh * p.G + g, req, len - n + i, there);
+  const int64_t pair = q.first + wave * 32 + col;
+  const bool there = pair < (int64_t)q.rows * p.G;
+  const int i = there ? (p.g_shift >= 0 ? (int)pair >> p.g_shift : (int)pair / p.G) : 0, g = there ? (int)(pair - (int64_t)i * p.G) : 0;
+  const SpanRow r = span_row(p, q.row0 + i, kvh * p.G + g, q.req, q.len - q.rows + i, there);
   // the last row's reach, and the keys all of the request's rows see
-  const int last = (int)(min(first + kSpanTile, (int64_t)n * p.G) - 1) / p.G;
-  int end = len - n + last + 1;
-  if (p.see_all) end = max(end, uniform(p.see_all[req]));
-  const SpanKeys keys{0, p.c.prefix_len, 0, clamped(end, 0, len), req, kvh};
-  typename S::State t;
-  auto part = [&](int stages, int x) { return (int)((int64_t)stages * x / p.splits); };
-  S span(p, keys, lds);
+  const int last_pair = (int)min(q.first + kSpanTile, (int64_t)q.rows * p.G) - 1, last = p.g_shift >= 0 ? last_pair >> p.g_shift : last_pair / p.G;
+  const int end = max(q.len - q.rows + last + 1, q.see_all);
+  S span(p, SpanKeys{0, p.c.prefix_len, 0, clamped(end, 0, q.len), q.req, kvh}, lds);
   const Survey<S> way(span, lds + S::LDS_ALL, r);
-  span.attend(part(span.stages, split), part(span.stages, split + 1), r, t, nullptr, way);
+  typename S::State t;
+  span.attend(part_start(span.stages, split, p.splits), part_start(span.stages, split + 1, p.splits), r, t, nullptr, way);
   span.store_rows(r, t, split);
 }
 
@@ -98,22 +103,22 @@ template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * 
     if (p.pre_wide) {
       const int pair = tile * 32 * NW + wave * 32 + col;
       const bool there = pair < all;
-      const int b = there ? pair / p.G : 0;
+      const int b = there ? (p.g_shift >= 0 ? pair >> p.g_shift : pair / p.G) : 0;
       const SpanRow r = span_row(p, b, kvh * p.G + (there ? pair - b * p.G : 0), b, span_len(p, b) - 1, there);
       Pre span(p, SpanKeys{0, p.c.prefix_len, 0, 0, 0, kvh}, lds);
       typename Pre::State t;
-      span.attend((int)((int64_t)span.stages * split / p.pre_splits), (int)((int64_t)span.stages * (split + 1) / p.pre_splits), r, t, nullptr, EveryStage{0x7fffffff});
+      span.attend(part_start(span.stages, split, p.pre_splits), part_start(span.stages, split + 1, p.pre_splits), r, t, nullptr, EveryStage{0x7fffffff});
       span.store_rows(r, t, split);
       return;
     }
     const int pair = tile * 32 + col;
     const bool there = pair < all;
-    const int b = there ? pair / p.G : 0;
+    const int b = there ? (p.g_shift >= 0 ? pair >> p.g_shift : pair / p.G) : 0;
     const SpanRow r = span_row(p, b, kvh * p.G + (there ? pair - b * p.G : 0), b, span_len(p, b) - 1, there);
     Own span(p, SpanKeys{0, p.c.prefix_len, 0, 0, 0, kvh}, lds);
     typename Own::State t;
-    span.attend((int)((int64_t)span.stages * split / p.pre_splits), (int)((int64_t)span.stages * (split + 1) / p.pre_splits), r, t, nullptr, EveryStage{0x7fffffff});
-    span.join_waves(t, min(32, all - tile * 32), tile * 32, split);
+    span.attend(part_start(span.stages, split, p.pre_splits), part_start(span.stages, split + 1, p.pre_splits), r, t, nullptr, EveryStage{0x7fffffff});
+    span.join_waves(t, r, min(32, all - tile * 32), split);
     return;
   }
   const int split = id % p.splits;
@@ -126,8 +131,8 @@ template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * 
   Own span(p, SpanKeys{0, 0, 0, len, b, kvh}, lds);
   typename Own::State t;
   float *scores = p.scores ? p.scores + (((int64_t)b * p.c.n_kv_heads + kvh) * p.G + (there ? g : 0)) * p.score_pitch : nullptr;
-  span.attend((int)((int64_t)span.stages * split / p.splits), (int)((int64_t)span.stages * (split + 1) / p.splits), r, t, scores, EveryStage{span.has_doc ? 0 : 0x7fffffff});
-  span.join_waves(t, rows, (int64_t)b * p.G + tile * 32, p.pre_splits + split);
+  span.attend(part_start(span.stages, split, p.splits), part_start(span.stages, split + 1, p.splits), r, t, scores, EveryStage{span.has_doc ? 0 : 0x7fffffff});
+  span.join_waves(t, r, rows, p.pre_splits + split);
 }
 
 // (maximum, sum) of a row's partial results, in every lane; mine: the weight of the result in slot `lane`, where there is one, over 2^maximum
@@ -153,7 +158,7 @@ __device__ __forceinline__ float2 slots_total(const SpanCall &p, int slots, int6
 // Partial results to results, a wave a row, V features a lane; all of a row's partial results are requested before the first is waited for.
 template <typename T, int V> __device__ __forceinline__ void join_row(const SpanCall &p, int slots, int64_t pair, int lane) {
   const int d = p.c.head_dim, f = lane * V;
-  const int64_t all = p.n_rows * p.nq, row = pair / p.nq;
+  const int64_t all = p.n_rows * p.nq, row = all >> 32 ? pair / p.nq : (int64_t)((unsigned)pair / (unsigned)p.nq);
   const int head = (int)(pair - row * p.nq);
   if (p.q_start && (row < p.q_start[0] || row >= p.q_start[p.c.n_requests])) return;  // no request's row
   float weight;
@@ -196,7 +201,7 @@ template <typename T, int V> __device__ __forceinline__ void join_row(const Span
 // The same for head sizes that neither two nor four features a lane fit.
 template <typename T> __device__ __forceinline__ void join_odd(const SpanCall &p, int slots, int64_t pair, int lane) {
   const int d = p.c.head_dim;
-  const int64_t all = p.n_rows * p.nq, row = pair / p.nq;
+  const int64_t all = p.n_rows * p.nq, row = all >> 32 ? pair / p.nq : (int64_t)((unsigned)pair / (unsigned)p.nq);
   const int head = (int)(pair - row * p.nq);
   if (p.q_start && (row < p.q_start[0] || row >= p.q_start[p.c.n_requests])) return;
   float weight;
@@ -522,11 +527,20 @@ template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> __global__ vo
 
 inline unsigned head_items(int heads, int items) { return 8u * ((unsigned)(heads >> 3) * items + ((unsigned)(heads & 7) * items + 7) / 8); }
 
-template <int NT, bool WIDE, typename K> hipError_t span_launch(K kernel, int lds, unsigned blocks, int threads, const SpanCall &p, hipStream_t s) {
+// most: LDS that any call of the kernel asks for; told to the device once
+template <auto K> hipError_t span_launch(int lds, int most, unsigned blocks, int threads, const SpanCall &p, hipStream_t s) {
+  static std::atomic<uint64_t> told{0};  // by device
   if (blocks == 0) return hipSuccess;
-  hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
   if (e != hipSuccess) return e;
-  kernel<<<blocks, threads, lds, s>>>(p);
+  const uint64_t bit = 1ull << (device & 63);
+  if (device > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void *)K, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e != hipSuccess) return e;
+    told.fetch_or(bit, std::memory_order_relaxed);
+  }
+  K<<<blocks, threads, lds, s>>>(p);
   return hipGetLastError();
 }
 
@@ -549,9 +563,8 @@ template <typename T> hipError_t span_prompt(const SpanCall &p, bool wide, hipSt
     constexpr int NT = decltype(nt)::value;
     constexpr bool W = decltype(w)::value;
     using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), 2, W>;
-    const int lds = S::LDS_ALL + (p.c.key_doc ? Survey<S>::LDS : 0);
-    return span_launch<NT, W>(k_span_prompt<T, NT, W>, lds,
-                              head_items(p.c.n_kv_heads, p.tiles * p.splits), 64 * kSpanWaves, p, s);
+    return span_launch<k_span_prompt<T, NT, W>>(S::LDS_ALL + (p.c.key_doc ? Survey<S>::LDS : 0), S::LDS_ALL + Survey<S>::LDS,
+                                                head_items(p.c.n_kv_heads, p.tiles * p.splits), 64 * kSpanWaves, p, s);
   });
 }
 
@@ -561,7 +574,8 @@ template <typename T> hipError_t span_token(const SpanCall &p, bool wide, hipStr
     constexpr bool W = decltype(w)::value;
     constexpr int NW = span_token_waves(NT, sizeof(T));
     constexpr int own = Span<T, NT, 1, NW, 32, 1, W>::LDS_ALL, pre = Span<T, NT, NW, 1, span_stage_keys(NT, sizeof(T)), 2, W>::LDS_ALL;
-    return span_launch<NT, W>(k_span_token<T, NT, W>, own > pre ? own : pre,
+    constexpr int lds = own > pre ? own : pre;
+    return span_launch<k_span_token<T, NT, W>>(lds, lds,
                               (unsigned)p.pre_items + (unsigned)p.c.n_requests * p.tiles * p.splits * p.c.n_kv_heads, 64 * NW, p, s);
   });
 }
@@ -577,7 +591,7 @@ template <typename T> hipError_t span_received(const SpanCall &p, bool wide, hip
       using R = Received<T, NT, W, ROWS, KB, NW>;
       const int blocks = (p.c.most + R::KEYS - 1) / R::KEYS, items = p.pairs_of_blocks ? (blocks + 1) / 2 : blocks;
       call.one_stage = p.last > 0 && (int64_t)p.last * p.G <= ROWS;
-      return span_launch<NT, W>(k_span_received<T, NT, W, ROWS, KB, NW>, call.one_stage ? R::LDS_ONE : R::LDS, head_items(p.c.n_kv_heads, items * p.c.n_requests), 64 * NW, call, s);
+      return span_launch<k_span_received<T, NT, W, ROWS, KB, NW>>(call.one_stage ? R::LDS_ONE : R::LDS, R::LDS, head_items(p.c.n_kv_heads, items * p.c.n_requests), 64 * NW, call, s);
     };
     using std::integral_constant;
     constexpr int few = CPR <= 32 ? 128 : 64;  // rows of a stage that fit LDS twice

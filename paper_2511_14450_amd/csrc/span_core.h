@@ -121,10 +121,11 @@ __device__ __forceinline__ int64_t own_offset(const hyp_attn_cache_t &c, int pag
   return (int64_t)page * page_stride + (int64_t)kvh * head_stride + (int64_t)(j & (c.page_keys - 1)) * key_stride;
 }
 
-// pair i of KV head c, counted from `first` over (row of q, head of the group), as (row of q) * nq + head
-__device__ inline int64_t pair_at(const SpanCall &p, int64_t first, int kvh, int i) {
-  const int64_t x = first + i, row = x / p.G;
-  return row * p.nq + kvh * p.G + (x - row * p.G);
+// stages [at(part), at(part + 1)) of `stages` are part `part` of `parts`
+__device__ __forceinline__ int part_start(int stages, int part, int parts) {
+  if (parts == 1) return part ? stages : 0;
+  const int each = stages / parts, more = stages - each * parts;
+  return part * each + min(part, more);
 }
 
 // RW waves of 32 rows each, KW waves that take turns at the keys; SKW keys of a wave in a stage; NBUF stages in LDS: with one, another
@@ -214,34 +215,37 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
       constexpr int LOADS = SKEYS * CPR / 64 / NW, ROWS = NW * 64 / CPR;  // rows between a lane's loads
       static_assert(LOADS * 64 * NW == SKEYS * CPR, "a stage is whole loads of all waves");
       const int first = (wave * 64 + lane) / CPR, piece = (wave * 64 + lane) % CPR;
-      const bool one_page = s.base + SKEYS <= s.end && !(s.own && small_page);
-      if (one_page) {
-        const T *start = base + uniform_offset<VALUES>(s);
-        constexpr bool SAME = ROWS % (KM + 1) == 0;  // all of a lane's rows exchange alike
-        const unsigned step = (unsigned)(ROWS * ks * ES);
+      constexpr bool SAME = ROWS % (KM + 1) == 0;  // all of a lane's rows exchange alike
+      auto fetch = [&](const char *src, int j, bool on) {
+        if (on) __builtin_amdgcn_global_load_lds((gbl_ptr_t *)src, (lds_ptr_t *)(dst + (j * NW + wave) * 1024), 16, 0, 0);
+      };
+      const bool one_page = !(s.own && small_page), whole = s.base + SKEYS <= s.end;
+      const unsigned row_bytes = (unsigned)(ks * ES);
+      if (one_page && whole) {
+        const char *start = (const char *)(base + uniform_offset<VALUES>(s));
+        const unsigned step = ROWS * row_bytes, here = (unsigned)first * row_bytes;
         const int c0 = piece ^ (VALUES ? vswz(first) : kswz(first));
-        const unsigned off0 = (unsigned)(first * ks * ES) + c0 * 16;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-          unsigned off = off0;
-          int c = c0;
-          if constexpr (!SAME) {
-            const int row = first + j * ROWS;
-            c = piece ^ (VALUES ? vswz(row) : kswz(row));
-            off = (unsigned)(first * ks * ES) + c * 16;
-          }
-          const char *src = (const char *)start + (size_t)j * step;
-          if (NT != 6 && chunks == CPR)
-            __builtin_amdgcn_global_load_lds((gbl_ptr_t *)(src + off), (lds_ptr_t *)(dst + (j * NW + wave) * 1024), 16, 0, 0);
-          else if (c < chunks)
-            __builtin_amdgcn_global_load_lds((gbl_ptr_t *)(src + off), (lds_ptr_t *)(dst + (j * NW + wave) * 1024), 16, 0, 0);
+          const int c = SAME ? c0 : piece ^ (VALUES ? vswz(first + j * ROWS) : kswz(first + j * ROWS));
+          const char *src = start + (size_t)j * step + (here + (unsigned)c * 16u);
+          if (NT != 6 && chunks == CPR) fetch(src, j, true);
+          else fetch(src, j, c < chunks);
+        }
+      } else if (KW > 1 && one_page) {
+        // the rows behind the last key are that key again, up to the end of its wave's block
+        const char *start = (const char *)(base + uniform_offset<VALUES>(s));
+        const int last = s.end - 1 - s.base, need = (last / SKW + 1) * SKW;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const int row = first + j * ROWS, c = piece ^ (VALUES ? vswz(row) : kswz(row));
+          fetch(start + ((unsigned)min(row, last) * row_bytes + (unsigned)c * 16u), j, c < chunks && row < need);
         }
       } else {
 #pragma unroll 1
         for (int j = 0; j < LOADS; ++j) {
           const int row = first + j * ROWS, c = piece ^ (VALUES ? vswz(row) : kswz(row));
-          const char *src = (const char *)(base + offset(min(s.base + row, s.end - 1))) + c * 16;
-          if (c < chunks) __builtin_amdgcn_global_load_lds((gbl_ptr_t *)src, (lds_ptr_t *)(dst + (j * NW + wave) * 1024), 16, 0, 0);
+          fetch((const char *)(base + offset(min(s.base + row, s.end - 1))) + c * 16, j, c < chunks);
         }
       }
     } else {
@@ -688,9 +692,8 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
       }
   }
 
-  // The waves that took turns at the keys of the same 32 rows, joined through LDS; rows: how many there are, row r being the
-  // pair (r / G, r % G) from `first` on.
-  __device__ __forceinline__ void join_waves(const State &t, int rows, int64_t first, int slot) const {
+  // The waves that took turns at the keys of the same rows, the lanes' r, joined through LDS.  rows: how many there are.
+  __device__ __forceinline__ void join_waves(const State &t, const SpanRow &info, int rows, int slot) const {
     static_assert(RW == 1, "rows of one wave");
     constexpr int PER = NDB * 32 * 33 + 64;
     float *mine = (float *)lds + wave * PER;
@@ -705,12 +708,11 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
     }
     __syncthreads();
     const int d = p.c.head_dim;
-    for (int i = threadIdx.x; i < rows * d; i += THREADS) {
-      const int row = i / d, f = i - row * d;
+    for (int row = wave; row < rows; row += NW) {  // a wave a row, a lane a feature
       float m = -INFINITY;
 #pragma unroll
       for (int w = 0; w < KW; ++w) m = fmaxf(m, ((float *)lds)[w * PER + row]);
-      float l = 0.f, o = 0.f, a[KW];
+      float l = 0.f, a[KW];
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float *x = (float *)lds + w * PER;
@@ -718,21 +720,24 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
         if (!is_zero(a[w])) l += a[w] * x[32 + row];
       }
       const float inv = 1.0f / l;
-#pragma unroll
-      for (int w = 0; w < KW; ++w)
-        if (!is_zero(a[w])) o += a[w] * inv * ((float *)lds)[w * PER + 64 + f * 33 + row];
-      const int64_t pair = pair_at(p, first, sg.kvh, row), r = pair / p.nq;
-      const int head = (int)(pair - r * p.nq);
-      if (p.part_o) {
-        const int64_t to = (int64_t)slot * p.n_rows * p.nq + pair;
-        p.part_o[to * d + f] = o;
-        if (f == 0) {
+      const int64_t r = __builtin_amdgcn_readlane(info.row, row);
+      const int head = __builtin_amdgcn_readlane(info.head, row);
+      const int64_t pair = r * p.nq + head, to = (int64_t)slot * p.n_rows * p.nq + pair;
+      if (lane == 0) {
+        if (p.part_o) {
           p.part_ml[2 * to] = is_zero(l) ? -INFINITY : m;
           p.part_ml[2 * to + 1] = l;
+        } else if (p.lse) {
+          p.lse[pair] = is_zero(l) ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
         }
-      } else {
-        store_f32((T *)p.out + r * p.out_rs + head * p.out_hs + f, o);
-        if (f == 0 && p.lse) p.lse[pair] = is_zero(l) ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      }
+      for (int f = lane; f < d; f += 64) {
+        float o = 0.f;
+#pragma unroll
+        for (int w = 0; w < KW; ++w)
+          if (!is_zero(a[w])) o += a[w] * inv * ((float *)lds)[w * PER + 64 + f * 33 + row];
+        if (p.part_o) p.part_o[to * d + f] = o;
+        else store_f32((T *)p.out + r * p.out_rs + head * p.out_hs + f, o);
       }
     }
   }

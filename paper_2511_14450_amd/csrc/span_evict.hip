@@ -17,6 +17,12 @@ __device__ __forceinline__ int64_t key_offset(const hyp_attn_cache_t &c, int shi
   return (int64_t)page * page_stride + (int64_t)kvh * head_stride + (int64_t)(j & (c.page_keys - 1)) * key_stride;
 }
 
+// Order of the keys as unsigned numbers: a NaN lowest, -0 as 0, what is always kept highest.
+__device__ __forceinline__ unsigned order_of(float total, bool always) {
+  const unsigned x = __float_as_uint(total);
+  return always ? 0xffffffffu : (x & 0x7fffffffu) > 0x7f800000u ? 0u : (x & 0x7fffffffu) == 0u ? 0x80000000u : x ^ ((x >> 31) ? 0xffffffffu : 0x80000000u);
+}
+
 // One request and KV head.  The keep-th largest total is found by three counts of 11, 11 and 10 bits; then one look at the totals in the
 // order of the slots says who stays (of equal totals the lowest slots), which slots become free and which keys move there.  A thread has
 // eight keys of each 8192, 1024 apart: up to so many keys are read once and stay in registers, more are read for every look.  Latency
@@ -36,7 +42,6 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
   const int *pos = p.c.key_pos ? p.c.key_pos + b * p.c.key_pos_request_stride + kvh * p.c.key_pos_head_stride : nullptr;
   const int64_t first = (int64_t)p.c.prefix_len + p.sink;
   const int64_t newest = (p.now ? (int64_t)p.now[b] : (int64_t)p.c.prefix_len + len) - p.recent;
-  // order of the keys as unsigned numbers: a NaN lowest, -0 as 0, what is always kept highest
   unsigned u[kItems];
   auto read = [&](int block) {
     float t[kItems];
@@ -48,12 +53,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
       at[i] = pos ? pos[j] : p.c.prefix_len + j;
     }
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const unsigned x = __float_as_uint(t[i]);
-      u[i] = at[i] < first || at[i] >= newest ? 0xffffffffu
-             : (x & 0x7fffffffu) > 0x7f800000u ? 0u
-             : (x & 0x7fffffffu) == 0u ? 0x80000000u : x ^ ((x >> 31) ? 0xffffffffu : 0x80000000u);
-    }
+    for (int i = 0; i < kItems; ++i) u[i] = order_of(t[i], at[i] < first || at[i] >= newest);
   };
   const bool once = len <= kBlock;
   if (once) read(0);
@@ -161,15 +161,70 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
   for (int i = tid; i < n_holes; i += kSelectThreads) kept[holes[i]] = moved[i];
 }
 
+// The same for up to 512 keys, and their move, in one launch: a key stays if fewer than `keep` come before it, counted one by one.
+constexpr int kSmall = 512;
+template <bool VEC, int ES> __device__ void move_rows(const EvictCall &p, int b, int kvh, int r0, int rows, const int *kept, int threads);
+
+template <bool VEC, int ES> __global__ void __launch_bounds__(kSmall) k_evict_small(const EvictCall p) {
+  __shared__ unsigned rank[kSmall];
+  __shared__ int from[kSmall], holes[kSmall], moved[kSmall], waves[2][kSmall / 64];
+  const int b = blockIdx.x / p.c.n_kv_heads, kvh = blockIdx.x % p.c.n_kv_heads, tid = threadIdx.x, K = p.keep, lane = tid & 63, wave = tid >> 6;
+  const int len = clamped(p.c.lens[b], 0, p.c.most);
+  int *kept = p.kept + (int64_t)blockIdx.x * K;
+  for (int r = tid; r < K; r += kSmall)
+    if (len <= K || r >= kSmall) kept[r] = r < len ? r : -1;
+  from[tid] = tid < len && tid < K ? tid : -1;
+  if (len > K) {
+    unsigned u = 0;
+    if (tid < len) {
+      const int at = p.c.key_pos ? p.c.key_pos[b * p.c.key_pos_request_stride + kvh * p.c.key_pos_head_stride + tid] : p.c.prefix_len + tid;
+      const int64_t newest = (p.now ? (int64_t)p.now[b] : (int64_t)p.c.prefix_len + len) - p.recent;
+      u = order_of(p.totals.in[b * p.totals.in_request_stride + kvh * p.totals.in_head_stride + tid], at < (int64_t)p.c.prefix_len + p.sink || at >= newest);
+    }
+    rank[tid] = u;
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < len; i += 4) {  // ranks behind the last key are 0 and come last
+      const uint4 x = *(const uint4 *)&rank[i];
+      before += (x.x > u || (x.x == u && i < tid)) + (x.y > u || (x.y == u && i + 1 < tid)) + (x.z > u || (x.z == u && i + 2 < tid)) + (x.w > u || (x.w == u && i + 3 < tid));
+    }
+    const bool stays = tid < len && before < K, hole = tid < K && !stays, mover = tid >= K && stays;
+    const unsigned long long hv = __ballot(hole), mv = __ballot(mover), below = (1ull << lane) - 1;
+    if (lane == 0) {
+      waves[0][wave] = __popcll(hv);
+      waves[1][wave] = __popcll(mv);
+    }
+    __syncthreads();
+    int h = __popcll(hv & below), m = __popcll(mv & below), n = 0;
+#pragma unroll
+    for (int w = 0; w < kSmall / 64; ++w) {
+      h += w < wave ? waves[0][w] : 0;
+      m += w < wave ? waves[1][w] : 0;
+      n += waves[0][w];
+    }
+    if (hole) holes[h] = tid;
+    if (mover) moved[m] = tid;
+    __syncthreads();
+    if (tid < n) from[holes[tid]] = moved[tid];
+    __syncthreads();
+    if (tid < K) kept[tid] = from[tid];
+  }
+  __syncthreads();
+  move_rows<VEC, ES>(p, b, kvh, 0, min(K, kSmall), from, kSmall);
+}
+
 // 32 slots of one request and KV head.
 template <bool VEC, int ES> __global__ void __launch_bounds__(256) k_evict_move(const EvictCall p) {
   const int per = (p.keep + kMoveRows - 1) / kMoveRows;
   const int pair = blockIdx.x / per, r0 = (blockIdx.x % per) * kMoveRows;
-  const int b = pair / p.c.n_kv_heads, kvh = pair % p.c.n_kv_heads, d = p.c.head_dim, rows = min(kMoveRows, p.keep - r0);
-  const int *kept = p.kept + (int64_t)pair * p.keep + r0;
-  // the kernel before was the last to read the old length
+  move_rows<VEC, ES>(p, pair / p.c.n_kv_heads, pair % p.c.n_kv_heads, r0, min(kMoveRows, p.keep - r0), p.kept + (int64_t)pair * p.keep + r0, 256);
+}
+
+// Rows r0 .. r0 + rows - 1 of the result: kept[r - r0] says where each comes from.
+template <bool VEC, int ES> __device__ void move_rows(const EvictCall &p, int b, int kvh, int r0, int rows, const int *kept, int threads) {
+  // what chose the keys was the last to read the old length
   if (kvh == 0 && r0 == 0 && threadIdx.x == 0) p.to.lens[b] = min(clamped(p.c.lens[b], 0, p.c.most), p.keep);
-  if (threadIdx.x < rows) {
+  if ((int)threadIdx.x < rows) {
     const int r = r0 + threadIdx.x, src = kept[threadIdx.x];
     if (src >= 0 && !(p.in_place && src == r)) {
       p.totals.out[b * p.totals.out_request_stride + kvh * p.totals.out_head_stride + r] =
@@ -182,8 +237,8 @@ template <bool VEC, int ES> __global__ void __launch_bounds__(256) k_evict_move(
             p.c.key_doc ? p.c.key_doc[b * p.c.key_doc_request_stride + kvh * p.c.key_doc_head_stride + src] : -1;
     }
   }
-  const int pieces = VEC ? d * ES / 16 : d;
-  for (int i = threadIdx.x; i < 2 * rows * pieces; i += 256) {
+  const int d = p.c.head_dim, pieces = VEC ? d * ES / 16 : d;
+  for (int i = threadIdx.x; i < 2 * rows * pieces; i += threads) {
     const bool v = i >= rows * pieces;
     const int x = v ? i - rows * pieces : i, row = x / pieces, at = x - row * pieces, src = kept[row];
     if (src < 0 || (p.in_place && src == r0 + row)) continue;
@@ -201,18 +256,21 @@ template <bool VEC, int ES> __global__ void __launch_bounds__(256) k_evict_move(
 
 }  // namespace
 
-hipError_t span_evict(const EvictCall &p, hipStream_t s) {
+template <bool VEC, int ES> static hipError_t evict(const EvictCall &p, hipStream_t s) {
   const unsigned pairs = (unsigned)p.c.n_requests * p.c.n_kv_heads;
-  k_evict_select<<<pairs, kSelectThreads, 0, s>>>(p);
-  const unsigned blocks = pairs * ((p.keep + kMoveRows - 1) / kMoveRows);
-  if (p.c.dtype == HYP_BF16) {
-    if (p.vec) k_evict_move<true, 2><<<blocks, 256, 0, s>>>(p);
-    else k_evict_move<false, 2><<<blocks, 256, 0, s>>>(p);
-  } else {
-    if (p.vec) k_evict_move<true, 4><<<blocks, 256, 0, s>>>(p);
-    else k_evict_move<false, 4><<<blocks, 256, 0, s>>>(p);
+  // In place the new lengths may be written only after all heads' workgroups have read the old ones: two launches.
+  if (!p.in_place && p.c.most <= kSmall) {
+    k_evict_small<VEC, ES><<<pairs, kSmall, 0, s>>>(p);
+    return hipGetLastError();
   }
+  k_evict_select<<<pairs, kSelectThreads, 0, s>>>(p);
+  k_evict_move<VEC, ES><<<pairs * ((p.keep + kMoveRows - 1) / kMoveRows), 256, 0, s>>>(p);
   return hipGetLastError();
+}
+
+hipError_t span_evict(const EvictCall &p, hipStream_t s) {
+  if (p.c.dtype == HYP_BF16) return p.vec ? evict<true, 2>(p, s) : evict<false, 2>(p, s);
+  return p.vec ? evict<true, 4>(p, s) : evict<false, 4>(p, s);
 }
 
 }  // namespace hyp

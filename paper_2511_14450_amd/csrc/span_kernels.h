@@ -62,7 +62,7 @@ hipError_t span_evict(const EvictCall &p, hipStream_t s);
 __host__ __device__ constexpr int span_steps(int d, bool wide) { return !wide ? (d <= 128 ? 8 : 16) : d <= 64 ? 4 : d <= 96 ? 6 : d <= 128 ? 8 : 16; }
 __host__ __device__ constexpr int span_chunks(int nt, int es) { return (nt == 6 ? 8 : nt) * es; }                 // 16-byte pieces of an LDS row
 __host__ __device__ constexpr int span_stage_keys(int nt, int es) { return es == 2 && nt <= 8 ? 64 : 32; }        // a wave's keys of a stage, waves by rows
-__host__ __device__ constexpr int span_token_waves(int nt, int es) { return span_chunks(nt, es) <= 16 ? 4 : span_chunks(nt, es) <= 32 ? 2 : 1; }
+__host__ __device__ constexpr int span_token_waves(int nt, int es) { return span_chunks(nt, es) <= 32 ? 4 : 2; }
 __host__ __device__ constexpr int span_steps_waves(int nt) { return nt <= 8 ? 2 : 1; }  // waves a SIMD that the registers are shared out for
 constexpr int kSpanWaves = 4;          // attn_prompt: waves of 32 rows
 constexpr int kSpanTile = 32 * kSpanWaves;
