@@ -38,6 +38,7 @@ __device__ __forceinline__ unsigned bits_of(float x) {
   return u;
 }
 __device__ __forceinline__ bool not_finite(float x) { return (bits_of(x) & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool is_nan(float x) { return (bits_of(x) & 0x7fffffffu) > 0x7f800000u; }
 __device__ __forceinline__ bool is_zero(float x) { return bits_of(x) == 0u; }
 __device__ __forceinline__ bool is_none(float x) { return bits_of(x) == 0xff800000u; }  // the maximum of no score
 // A value the compiler does not know to be the same in the next trip of a loop: what is formed of it is formed again there, instead of
@@ -551,25 +552,40 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
   }
 
   // A value that a row does not see is multiplied by a probability of zero; if it is an infinity or a NaN that is no zero.  Then, as
-  // where a sum leaves the range of a float although the result does not, a wave's rows are summed again one key at a time, with
-  // their final weights, from memory.  Slow, and right.  The result is the one of a sum of one.
+  // where a sum leaves the range of a float although the result does not, those features of a wave's rows that are not finite are summed
+  // again one key at a time, with the rows' final weights, from memory: slow, and right.  It ends as soon as all of them are NaN, which
+  // no key undoes; a row whose sum of weights is none has only NaN from the start.  The result is the one of a sum of one.
   __device__ __forceinline__ void careful(int st0, int st1, const SpanRow &r, State &t) const {
     const int kw = KW > 1 ? wave / RW : 0, d = p.c.head_dim;
-    if (!is_zero(t.l)) {
+    const bool none = is_zero(t.l), lost = not_finite(t.l);
+    if (lost) t.m = t.l;  // whatever this part is joined with
+    const bool sums = r.there && !none && !lost;
+    const float inv = sums ? 1.0f / t.l : 1.0f;
+    if (sums) {
       t.m += __builtin_amdgcn_logf(t.l);
       t.l = 1.0f;
     }
+    unsigned again[NDB];  // a bit for each feature that is summed again
+    bool open = false;    // whether some of them is not NaN yet
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      again[db] = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const bool odd = sums && not_finite(t.o[db][i]);
+        if (odd && 32 * db + key_of(i, hh) < d) again[db] |= 1u << i;
+        t.o[db][i] = odd || none ? 0.f : t.o[db][i] * inv;
+      }
+      open |= again[db] != 0;
+    }
     const float m = t.m;
     const T *q = row_q<T>(p, r);
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t.o[db][i] = 0.f;
     for (int st = st0; st < st1; ++st) {
       const Stage sta = stage_of(st);
       const int base = sta.base + kw * SKW, end = min(base + SKW, sta.end);
       for (int key = base; key < end; ++key) {
-        bool seen = r.there && (!sta.own || key <= r.lim);
+        if (!__any(open)) return;
+        bool seen = open && (!sta.own || key <= r.lim);
         int64_t ko, vo;
         int pos = key;
         if (sta.own) {
@@ -585,21 +601,25 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
           ko = sg.kvh * p.c.prefix_k_head_stride + key * p.c.prefix_k_key_stride;
           vo = sg.kvh * p.c.prefix_v_head_stride + key * p.c.prefix_v_key_stride;
         }
-        if (!seen || is_zero(t.l)) continue;
-        const T *k = (const T *)(sta.own ? p.c.k : p.c.prefix_k) + ko, *v = (const T *)(sta.own ? p.c.v : p.c.prefix_v) + vo;
-        float dot = 0.f;
-        for (int f = 0; f < d; ++f) dot = fmaf(load_val(q + f), load_val(k + f), dot);
-        dot = p.cap2 != 0.f ? cap_any(dot, p.cap_c, p.cap_most, p.to_cap, p.cap2) : dot * p.scale2;
-        if (p.slopes) dot -= r.slope2 * fabsf((float)(r.pos - pos));
-        const float pr = exp2_(dot - m);
-        if (is_zero(pr)) continue;
+        if (seen) {
+          const T *k = (const T *)(sta.own ? p.c.k : p.c.prefix_k) + ko, *v = (const T *)(sta.own ? p.c.v : p.c.prefix_v) + vo;
+          float dot = 0.f;
+          for (int f = 0; f < d; ++f) dot = fmaf(load_val(q + f), load_val(k + f), dot);
+          dot = p.cap2 != 0.f ? cap_any(dot, p.cap_c, p.cap_most, p.to_cap, p.cap2) : dot * p.scale2;
+          if (p.slopes) dot -= r.slope2 * fabsf((float)(r.pos - pos));
+          const float pr = exp2_(dot - m);
+          if (!is_zero(pr)) {
+            open = false;
 #pragma unroll
-        for (int db = 0; db < NDB; ++db)
+            for (int db = 0; db < NDB; ++db)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int f = 32 * db + key_of(i, hh);
-            if (f < d) t.o[db][i] = fmaf(pr, load_val(v + f), t.o[db][i]);
+              for (int i = 0; i < 16; ++i)
+                if (again[db] >> i & 1) {
+                  t.o[db][i] = fmaf(pr, load_val(v + 32 * db + key_of(i, hh)), t.o[db][i]);
+                  open |= !is_nan(t.o[db][i]);
+                }
           }
+        }
       }
     }
   }
