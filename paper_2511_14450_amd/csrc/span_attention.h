@@ -152,7 +152,7 @@ __device__ __forceinline__ float2 slots_total(const SpanCall &p, int slots, int6
   }
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
-  return {m, l};
+  return {not_finite(l) ? l : m, l};  // a maximum passes over NaN
 }
 
 // Partial results to results, a wave a row, V features a lane; all of a row's partial results are requested before the first is waited for.
@@ -507,7 +507,7 @@ template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> struct Receiv
   }
 };
 
-template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> __global__ void __launch_bounds__(64 * NW, NW == 4 && NT <= 8 && sizeof(T) == 2 ? 3 : 2) k_span_received(const SpanCall p) {
+template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> __global__ void __launch_bounds__(64 * NW, NW == 4 && NT <= 8 && sizeof(T) == 2 ? 3 : NW == 4 && span_chunks(NT, sizeof(T)) > 32 ? 1 : 2) k_span_received(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using R = Received<T, NT, WIDE, ROWS, KB, NW>;
   const int blocks = (p.c.most + R::KEYS - 1) / R::KEYS, items = p.pairs_of_blocks ? (blocks + 1) / 2 : blocks;

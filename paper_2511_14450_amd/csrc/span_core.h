@@ -237,7 +237,7 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
         // the rows behind the last key are that key again, up to the end of its wave's block
         const char *start = (const char *)(base + uniform_offset<VALUES>(s));
         const int last = s.end - 1 - s.base, need = (last / SKW + 1) * SKW;
-#pragma unroll
+#pragma unroll(LOADS > 8 ? 4 : LOADS)  // the widest rows have 32 loads, whose addresses do not fit the registers
         for (int j = 0; j < LOADS; ++j) {
           const int row = first + j * ROWS, c = piece ^ (VALUES ? vswz(row) : kswz(row));
           fetch(start + ((unsigned)min(row, last) * row_bytes + (unsigned)c * 16u), j, c < chunks && row < need);
@@ -555,7 +555,7 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
   // where a sum leaves the range of a float although the result does not, those features of a wave's rows that are not finite are summed
   // again one key at a time, with the rows' final weights, from memory: slow, and right.  It ends as soon as all of them are NaN, which
   // no key undoes; a row whose sum of weights is none has only NaN from the start.  The result is the one of a sum of one.
-  __device__ __forceinline__ void careful(int st0, int st1, const SpanRow &r, State &t) const {
+  template <typename Way> __device__ __forceinline__ void careful(int st0, int st1, const SpanRow &r, State &t, const Way &way) const {
     const int kw = KW > 1 ? wave / RW : 0, d = p.c.head_dim;
     const bool none = is_zero(t.l), lost = not_finite(t.l);
     if (lost) t.m = t.l;  // whatever this part is joined with
@@ -580,7 +580,7 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
     }
     const float m = t.m;
     const T *q = row_q<T>(p, r);
-    for (int st = st0; st < st1; ++st) {
+    for (int st = way.next(st0, st1); st < st1; st = way.next(st + 1, st1)) {
       const Stage sta = stage_of(st);
       const int base = sta.base + kw * SKW, end = min(base + SKW, sta.end);
       for (int key = base; key < end; ++key) {
@@ -654,7 +654,7 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) odd |= not_finite(t.o[db][i]);
-    if (__any(odd && r.there)) careful(st0, st1, r, t);
+    if (__any(odd && r.there)) careful(st0, st1, r, t, way);
   }
 
   // A row's result straight from its registers: normalised, or as partial result of `slot`.
@@ -745,7 +745,7 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
       const int64_t pair = r * p.nq + head, to = (int64_t)slot * p.n_rows * p.nq + pair;
       if (lane == 0) {
         if (p.part_o) {
-          p.part_ml[2 * to] = is_zero(l) ? -INFINITY : m;
+          p.part_ml[2 * to] = is_zero(l) ? -INFINITY : not_finite(l) ? l : m;  // a maximum passes over NaN
           p.part_ml[2 * to + 1] = l;
         } else if (p.lse) {
           p.lse[pair] = is_zero(l) ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;

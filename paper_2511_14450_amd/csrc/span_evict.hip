@@ -17,10 +17,12 @@ __device__ __forceinline__ int64_t key_offset(const hyp_attn_cache_t &c, int shi
   return (int64_t)page * page_stride + (int64_t)kvh * head_stride + (int64_t)(j & (c.page_keys - 1)) * key_stride;
 }
 
-// Order of the keys as unsigned numbers: a NaN lowest, -0 as 0, what is always kept highest.
-__device__ __forceinline__ unsigned order_of(float total, bool always) {
+// Order of the keys as unsigned numbers: a NaN lowest, -0 as 0, what is always kept highest.  Where more are always kept than there is
+// room for (positions say so, which are the caller's), only those count, in the order of their totals.
+__device__ __forceinline__ unsigned order_of(float total, bool always, bool crowded) {
   const unsigned x = __float_as_uint(total);
-  return always ? 0xffffffffu : (x & 0x7fffffffu) > 0x7f800000u ? 0u : (x & 0x7fffffffu) == 0u ? 0x80000000u : x ^ ((x >> 31) ? 0xffffffffu : 0x80000000u);
+  const unsigned order = (x & 0x7fffffffu) > 0x7f800000u ? 1u : (x & 0x7fffffffu) == 0u ? 0x80000000u : x ^ ((x >> 31) ? 0xffffffffu : 0x80000000u);
+  return crowded ? (always ? order : 0u) : (always ? 0xffffffffu : order);
 }
 
 // One request and KV head.  The keep-th largest total is found by three counts of 11, 11 and 10 bits; then one look at the totals in the
@@ -43,6 +45,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
   const int64_t first = (int64_t)p.c.prefix_len + p.sink;
   const int64_t newest = (p.now ? (int64_t)p.now[b] : (int64_t)p.c.prefix_len + len) - p.recent;
   unsigned u[kItems];
+  bool crowded = false;
   auto read = [&](int block) {
     float t[kItems];
     int at[kItems];
@@ -53,7 +56,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
       at[i] = pos ? pos[j] : p.c.prefix_len + j;
     }
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) u[i] = order_of(t[i], at[i] < first || at[i] >= newest);
+    for (int i = 0; i < kItems; ++i) u[i] = order_of(t[i], at[i] < first || at[i] >= newest, crowded);
   };
   const bool once = len <= kBlock;
   if (once) read(0);
@@ -91,6 +94,12 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
       found[1] = need - above - own0;
     }
     __syncthreads();
+    if (look == 0 && found[0] == 2047 && !crowded) {  // only what is always kept is up there
+      crowded = true;
+      if (once) read(0);
+      look = -1;
+      continue;
+    }
     prefix |= (unsigned)found[0] << shift;
     mask |= (unsigned)(bins - 1) << shift;
     need = found[1];
@@ -176,13 +185,21 @@ template <bool VEC, int ES> __global__ void __launch_bounds__(kSmall) k_evict_sm
   from[tid] = tid < len && tid < K ? tid : -1;
   if (len > K) {
     unsigned u = 0;
+    bool always = false;
+    float total = 0.f;
     if (tid < len) {
       const int at = p.c.key_pos ? p.c.key_pos[b * p.c.key_pos_request_stride + kvh * p.c.key_pos_head_stride + tid] : p.c.prefix_len + tid;
       const int64_t newest = (p.now ? (int64_t)p.now[b] : (int64_t)p.c.prefix_len + len) - p.recent;
-      u = order_of(p.totals.in[b * p.totals.in_request_stride + kvh * p.totals.in_head_stride + tid], at < (int64_t)p.c.prefix_len + p.sink || at >= newest);
+      total = p.totals.in[b * p.totals.in_request_stride + kvh * p.totals.in_head_stride + tid];
+      always = at < (int64_t)p.c.prefix_len + p.sink || at >= newest;
+      u = order_of(total, always, false);
     }
     rank[tid] = u;
-    __syncthreads();
+    if (__syncthreads_count(always) > K) {
+      u = tid < len ? order_of(total, always, true) : 0u;
+      rank[tid] = u;
+      __syncthreads();
+    }
     int before = 0;
     for (int i = 0; i < len; i += 4) {  // ranks behind the last key are 0 and come last
       const uint4 x = *(const uint4 *)&rank[i];
