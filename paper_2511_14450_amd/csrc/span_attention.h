@@ -168,18 +168,25 @@ template <typename T, int V> __device__ __forceinline__ void join_row(const Span
   const float inv = none ? 0.f : 1.0f / ml.y;
   float acc[V] = {};
   const bool on = f < d;  // V divides d
-  for (int s0 = 0; s0 < slots; s0 += 8) {
+  // slots that hold something: those of the first 64 by a look at their weights, which all lanes have; an empty slot holds nothing, not
+  // even zeros
+  unsigned long long live = __ballot(!is_zero(weight));
+  for (int next = 64; live || next < slots;) {
     float o[8][V], w[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int s = s0 + u;
       w[u] = 0.f;
+      int s = slots;
+      if (live) {
+        s = __builtin_ctzll(live);
+        live &= live - 1;
+        w[u] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s));
+      } else if (next < slots) {
+        s = next++;
+        const float2 x = ((const float2 *)p.part_ml)[s * all + pair];
+        w[u] = is_none(x.x) ? 0.f : exp2_(x.x - ml.x) * x.y;
+      }
       if (s < slots) {
-        if (s < 64) w[u] = __shfl(weight, s);
-        else {
-          const float2 x = ((const float2 *)p.part_ml)[s * all + pair];
-          w[u] = is_none(x.x) ? 0.f : exp2_(x.x - ml.x) * x.y;
-        }
         const float *src = p.part_o + (s * all + pair) * d + f;
 #pragma unroll
         for (int e = 0; e < V; ++e) o[u][e] = on ? src[e] : 0.f;
@@ -187,7 +194,7 @@ template <typename T, int V> __device__ __forceinline__ void join_row(const Span
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      if (!is_zero(w[u])) {  // an empty slot holds nothing, not even zeros
+      if (!is_zero(w[u])) {
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = fmaf(w[u] * inv, o[u][e], acc[e]);
       }
