@@ -15,7 +15,7 @@ struct SpanCall {
   int g_shift;                // log2(G), -1: G is no power of two
   float scale2;               // scale * log2(e): scores are held as exponents of two
   float to_cap, cap2;         // scale / cap, cap * log2(e); cap2 0: not capped
-  float cap_c[5], cap_most;   // polynomial of the capped score, and the largest raw score it is for
+  float cap_c[4], cap_most;   // polynomial of the capped score, and the largest raw score it is for
   const float *slopes;
   const void *q;
   int64_t q_rs, q_hs;
