@@ -21,7 +21,8 @@ FLAGS = [
 ]
 
 
-# per-file additions: the attention kernels take maxima over MFMA results that are never NaN
+# per-file additions: the attention kernels take maxima over MFMA results; those of span_*.hip, which promise what NaN does, look at numbers
+# that may be NaN by their bits
 EXTRA_FLAGS = {name: ["-fno-honor-nans"] for name in ("mfma_attention.hip", "span_bf16.hip", "span_f32.hip")}
 
 

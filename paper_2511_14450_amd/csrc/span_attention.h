@@ -15,7 +15,7 @@ namespace {
 struct TileRequest { int req, row0, rows, len, see_all; int64_t first; };  // first: the tile's first pair inside the request, -1: none
 
 // Request b's tiles start at floor(q_start[b] G / tile) + b, which leaves each as many as it needs, or one more.  The lanes look at 64
-// requests each, all that is to be known of them requested at once: one after the other these loads were a third of a small call's time.
+// requests each, all that is to be known of them requested at once, where a bisection has a round trip to memory for each halving.
 __device__ __forceinline__ TileRequest tile_request(const SpanCall &p, int t, int tile) {
   const int n = p.c.n_requests, lane = threadIdx.x & 63;
   auto cut = [&](int v) { return (int)min(max((int64_t)v, (int64_t)0), p.n_rows); };
@@ -59,7 +59,12 @@ __device__ __forceinline__ bool head_item(int id, int heads, int items, int &hea
 }
 
 // attn_prompt.  A workgroup: one KV head, rows of one request (dense over the group's heads), all the keys they see or one of `splits` parts
-// of them: 128 rows, 32 a wave, whose waves meet the same keys.
+// of them: 128 rows, 32 a wave, whose waves meet the same keys.  Two workgroups a CU, so that one's softmax runs beside the other's
+// products; keys and values of the next stage are fetched straight into LDS meanwhile.  A score costs about thirteen vector instructions
+// (two of them its exponential's and sum's, five a cap's) and a 16th of a matrix instruction for each 16 features: with 128 features the
+// vector unit is busy for 0.55 of the time and the matrix unit for 0.3, and the two overlap less than half.  4 x 8192 causal rows of 40 heads of 128
+// bf16 features: 3.8 ms capped (0.73 PFLOP/s), 3.2 ms not.  Tiles of 32 rows whose waves share the keys, for calls of few tiles:
+// 920 f32 rows took 58 us, these 42, since each tile fetches the keys again.
 template <typename T, int NT, bool WIDE>
 __global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_prompt(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -85,7 +90,10 @@ __global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_
 }
 
 // attn_token.  Items over the shared keys, which all requests' rows meet at once, then items of up to 32 rows of one request
-// over its own keys, whose waves take turns at them.
+// over its own keys, whose waves take turns at them.  The keys' bytes bound it: 8 requests of 9216 own keys, 8 heads of 128 bf16 features in
+// pages of 128, take 54 us, 5.5 TB/s.  With one stage in LDS two workgroups fit a CU, and one's loads run beside the other's products; two
+// stages and one workgroup took 86 us.  32 requests behind 8192 shared keys, 10 heads: 30 us, 2.9 TB/s - there the items are short, and a
+// third of their time is the way to the first key and from the last.
 template <typename T, int NT, bool WIDE> __global__ void __launch_bounds__(64 * span_token_waves(NT, sizeof(T)), span_steps_waves(NT)) k_span_token(const SpanCall p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   constexpr int NW = span_token_waves(NT, sizeof(T));
@@ -155,7 +163,8 @@ __device__ __forceinline__ float2 slots_total(const SpanCall &p, int slots, int6
   return {not_finite(l) ? l : m, l};  // a maximum passes over NaN
 }
 
-// Partial results to results, a wave a row, V features a lane; all of a row's partial results are requested before the first is waited for.
+// Partial results to results, a wave a row, V features a lane; eight of a row's partial results are requested before the first is waited for.
+// Bytes bound it: seven parts of 920 f32 rows of 8 heads of 128 features take 8 us, 18 of 32 bf16 requests with their totals 6.6 us.
 template <typename T, int V> __device__ __forceinline__ void join_row(const SpanCall &p, int slots, int64_t pair, int lane) {
   const int d = p.c.head_dim, f = lane * V;
   const int64_t all = p.n_rows * p.nq, row = all >> 32 ? pair / p.nq : (int64_t)((unsigned)pair / (unsigned)p.nq);
@@ -285,7 +294,10 @@ template <typename T> __global__ void __launch_bounds__(256) k_span_join(const S
 // that all workgroups have about the same number of rows to meet.  Half of its NW waves hold one half of the keys in registers, half the
 // other; a head's rows pass by through LDS, ROWS at a time, from the last to the first, so that the workgroups of an XCD meet the same rows
 // at about the same time.  What a key gets is summed in its lane over the rows, then over lanes and waves, in a fixed order.
-// Rows come from L2 for every block of keys: 64 keys of 128 bf16 features to a block made that the bound (4.5 TB/s).
+// Rows come from L2 for every block of keys: 64 keys of 128 bf16 features to a block made that the bound (4.5 TB/s), and 6007 capped rows of
+// 40 heads took 1.7 ms; with 128 keys it is the vector unit, as in attn_prompt at half the products a score, and 0.45 ms (0.41 PFLOP/s).
+// Where few rows count (8 requests, their last 32 rows, 12 K keys) there is a stage to a workgroup, 26 us for two rounds of workgroups
+// that each wait for their keys.
 template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> struct Received {
   using S = Span<T, NT, NW, 1, 32, 1, WIDE>;
   static constexpr int ES = sizeof(T), EPC = 16 / ES, KEYS = 64 * KB, THREADS = 64 * NW, TILE = ROWS * S::ROWB;
