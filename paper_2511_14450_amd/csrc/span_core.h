@@ -603,6 +603,7 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
         if (seen) {
           const T *k = (const T *)(sta.own ? p.c.k : p.c.prefix_k) + ko, *v = (const T *)(sta.own ? p.c.v : p.c.prefix_v) + vo;
           float dot = 0.f;
+#pragma unroll 8  // so many features' loads at once; the values' would not find registers
           for (int f = 0; f < d; ++f) dot = fmaf(load_val(q + f), load_val(k + f), dot);
           dot = p.cap2 != 0.f ? cap_any(dot, p.cap_c, p.cap_most, p.to_cap, p.cap2) : dot * p.scale2;
           if (p.slopes) dot -= r.slope2 * fabsf((float)(r.pos - pos));
