@@ -170,9 +170,9 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
   for (int i = tid; i < n_holes; i += kSelectThreads) kept[holes[i]] = moved[i];
 }
 
-// The same for up to 512 keys, and their move, in one launch: a key stays if fewer than `keep` come before it, counted one by one.  Latency
-// bounds it, 8 us for caches of 96 keys; in two launches a call took 17 us, in one 12.
-constexpr int kSmall = 512;
+// The same for up to 256 keys, and their move, in one launch: a key stays if fewer than `keep` come before it, counted one by one.  Latency
+// bounds it, 8 us for caches of 96 keys.  A call takes 13 us for 96 keys, 17 for 256; in two launches 17 for either, and for 512 (25 in one).
+constexpr int kSmall = 256;
 template <bool VEC, int ES> __device__ void move_rows(const EvictCall &p, int b, int kvh, int r0, int rows, const int *kept, int threads);
 
 template <bool VEC, int ES> __global__ void __launch_bounds__(kSmall) k_evict_small(const EvictCall p) {

@@ -88,3 +88,24 @@ def test_parts_whose_sums_are_lost_meet_parts_that_are_not():
     q, *_ = pr.device()
     out, lse = hyp.attn_token(pr.cache, pr.rule, q)
     assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+
+
+@pytest.mark.parametrize("most", [255, 256, 257])
+def test_eviction_in_one_launch_and_in_two(most):
+    for totals in ("heavy", "ties", "odd"):
+        check_evict(BF, [most, most // 2, most - 1, 0], 2, 64, (most + 1) // 2, recent=3, totals=totals, room=most)
+        check_evict(F32, [most, 3], 1, 33, most - 2, totals=totals, room=most, page=64, pos=True, doc=True, prefix=9)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [1, 2, 4, 5, 8, 9])
+def test_rows_at_the_shared_keys_around_a_wave(dtype, n):
+    check_token(Problem(n, dtype, 4, 1, 64, held=[5 + 9 * b for b in range(n)], prefix=300))
+
+
+def test_received_weight_by_pairs_of_blocks_and_by_blocks():
+    # 160 pairs of blocks: the weight of many prompts of one key head, and of one less
+    for n in (160, 159):
+        held = [(17 * b) % 40 + 1 for b in range(n)]
+        held[3] = 140
+        check_prompt(Problem(n, BF, 5, 1, 40, held=held, rows=[min(h, 30) for h in held]), last=0)
