@@ -17,9 +17,10 @@ inline int span_prompt_splits(int64_t workgroups, int64_t stages, int64_t fewest
 struct SpanTokenPlan { int pre_wide, pre_tiles, pre_splits, tiles, splits; };
 
 // attn_token: parts of an even share of all keys for 512 workgroups.  32 requests of 100 to 608 keys behind 8192 take 37 us so; with half,
-// 0.75, 1.5 and twice as many parts of the shared keys 45, 38, 40 and 43 us, with 0.75 and 1.5 times those of the own ones 44 and 37 us (8 requests
-// of 9216 keys: 68 and 73 instead of 60 us).  Of up to 16 rows the waves
-// share the shared keys (2 requests of 4 heads a group: 25 us, a wave for each 32 rows 28), more have a wave for each 32 (4 requests 28 either way, 8: 33 and 28).  waves: of a workgroup; pre_stage: keys of a stage of items over the shared keys where each wave has rows of its own
+// 0.75, 1.5 and twice as many parts of the shared keys 45, 38, 40 and 43 us, with 0.75 and 1.5 times those of the own ones 44 and 37 us
+// (8 requests of 9216 keys: 68 and 73 instead of 60 us).  Of up to 16 rows the waves share the shared keys (2 requests of 4 heads a group:
+// 25 us, a wave for each 32 rows 28), more have a wave for each 32 (4 requests 28 either way, 8: 33 and 28).
+// waves: of a workgroup; pre_stage: keys of a stage of items over the shared keys where each wave has rows of its own
 inline SpanTokenPlan span_token_plan(int64_t requests, int64_t kv_heads, int64_t group, int64_t most, int64_t prefix, int waves, int pre_stage) {
   SpanTokenPlan t = {};
   const int64_t rows = requests * group;
