@@ -54,7 +54,11 @@ __device__ __forceinline__ int wave_min(int v) {
   for (int s = 1; s < 64; s <<= 1) v = min(v, __shfl_xor(v, s));
   return v;
 }
-__device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
+__device__ __forceinline__ int wave_max(int v) {  // not the negated minimum: -2^31, which is an id as well, has no negative
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) v = max(v, __shfl_xor(v, s));
+  return v;
+}
 __device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 // A raw score S as an exponent of two, cap log2(e) tanh(S scale / cap).  With x = S scale / cap up to 0.4 in absolute value that is
