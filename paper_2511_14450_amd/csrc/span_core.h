@@ -104,7 +104,7 @@ __device__ __forceinline__ SpanRow span_row(const SpanCall &p, int row, int head
   r.row = row;
   r.head = head;
   r.lim = own_index;
-  if (there && p.see_all && p.q_start) r.lim = max(r.lim, p.see_all[req] - 1);
+  if (there && p.see_all && p.q_start) r.lim = max(r.lim, max(p.see_all[req], 0) - 1);  // no less than none: -2^31 has no predecessor
   r.doc = there && p.c.key_doc && p.q_doc ? p.q_doc[row] : -1;
   r.pos = there && p.q_pos ? p.q_pos[row] : p.c.prefix_len + own_index;
   r.slope2 = there && p.slopes ? p.slopes[head] * kLog2e : 0.f;

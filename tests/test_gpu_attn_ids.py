@@ -1,4 +1,4 @@
-"""Ids at the end of their range: every negative id sees and is seen by all, -2^31 too."""
+"""Ids and counts at the end of their range: every negative id sees and is seen by all, -2^31 too, and a count of none shows nothing."""
 import pytest
 import torch
 
@@ -30,3 +30,8 @@ def test_the_least_id_is_one_that_sees_all(dtype, of):
     tok = documents(dtype, 32, rows=None)
     tok.q_doc[0], tok.key_doc[:, :, 12] = LEAST, LEAST
     check_token(tok)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_least_count_shows_nothing(dtype):
+    check_prompt(Problem(33, dtype, 4, 2, 64, held=[150, 90], rows=[150, 40], prefix=10, see_all=[LEAST, LEAST + 1]))
