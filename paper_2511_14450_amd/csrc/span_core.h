@@ -12,7 +12,7 @@
 namespace hyp {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = (float)(1.4426950408889634 - (double)kLog2e), kLn2 = 0.6931471805599453f;
 constexpr float kFollow = 8.0f;  // the running maximum moves when a score passes it by more than 2^8
 
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16v4_t;
