@@ -1,5 +1,6 @@
 // C entry points of hyp_attn.h: checks of the arguments and the cut of a call into launches.
 #include <cmath>
+#include <limits>
 #include <new>
 #include <string>
 
@@ -110,7 +111,7 @@ void add_rule(SpanCall &p, const hyp_attn_rule_t &rule) {
   constexpr float log2e = 1.4426950408889634f;
   p.scale2 = rule.scale * log2e;
   if (rule.cap > 0.f) {
-    p.to_cap = rule.scale / rule.cap;
+    p.to_cap = std::min(rule.scale / rule.cap, std::numeric_limits<float>::max());  // a score of 0 stays one under the smallest caps
     p.cap2 = rule.cap * log2e;
     // tanh(x) / x in powers of x^2 up to |x| = 0.4, of least relative error (9.8e-8); up to 0.5 the same error takes a power more, and an
     // instruction more of the thirteen that a score costs
