@@ -73,7 +73,7 @@ typedef struct {
 } hyp_attn_cache_t;
 
 typedef struct {
-  float scale;           /* > 0                                                       */
+  float scale;           /* > 0; below 2.3e38 if scores are not capped                */
   float cap;             /* 0: scores are not capped                                  */
   const float *slopes;   /* [n_q_heads] or null                                       */
 } hyp_attn_rule_t;

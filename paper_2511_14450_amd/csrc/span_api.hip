@@ -11,6 +11,7 @@ namespace hyp {
 namespace {
 
 thread_local std::string t_error;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct Refused {
   hyp_status_t status;
@@ -54,6 +55,7 @@ void check_rule(const hyp_attn_rule_t *r) {
   need(r, HYP_EINVAL, "rule is null");
   need(std::isfinite(r->scale) && r->scale > 0.f, HYP_EINVAL, "rule: scale must be finite and positive");
   need(std::isfinite(r->cap) && r->cap >= 0.f, HYP_EINVAL, "rule: cap must be finite and not negative");
+  need(r->cap > 0.f || std::isfinite(r->scale * kLog2e), HYP_EINVAL, "rule: scale must be below 2.3e38 where scores are not capped");
 }
 
 void check_rows(const hyp_attn_cache_t &c, const hyp_attn_rows_t *r, bool token) {
@@ -108,16 +110,15 @@ SpanCall begin(const hyp_attn_cache_t &c, const hyp_attn_rows_t &r) {
 }
 
 void add_rule(SpanCall &p, const hyp_attn_rule_t &rule) {
-  constexpr float log2e = 1.4426950408889634f;
-  p.scale2 = rule.scale * log2e;
+  p.scale2 = rule.scale * kLog2e;
   if (rule.cap > 0.f) {
     p.to_cap = std::min(rule.scale / rule.cap, std::numeric_limits<float>::max());  // a score of 0 stays one under the smallest caps
-    p.cap2 = rule.cap * log2e;
+    p.cap2 = rule.cap * kLog2e;
     // tanh(x) / x in powers of x^2 up to |x| = 0.4, of least relative error (9.8e-8); up to 0.5 the same error takes a power more, and an
     // instruction more of the thirteen that a score costs
     constexpr double tanh_c[4] = {0.9999999019048974, -0.3333136247072489, 0.13270976813015187, -0.04755360235665809};
     const double k = (double)rule.scale / rule.cap;
-    double f = (double)rule.scale * log2e;
+    double f = (double)rule.scale * kLog2e;
     for (int i = 0; i < 4; ++i, f *= k * k) p.cap_c[i] = (float)(f * tanh_c[i]);
     p.cap_most = (float)(0.4 / k);
     if (!std::isfinite(p.cap_c[3])) p.cap_most = -1.f;  // a cap so far below the scale that tanh is 0 or 1

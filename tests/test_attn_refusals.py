@@ -1,0 +1,16 @@
+"""Arguments that include/hyp_attn.h refuses before anything touches the device, and that the binding does; needs no GPU."""
+import ctypes as C
+
+import pytest
+
+from paper_2511_14450_amd import attn, binding
+from tests.test_attn_host import OUT, TOTALS, cache, calls, rows
+
+EINVAL, ESHAPE, ENOMEM = binding.HYP_EINVAL, binding.HYP_ESHAPE, binding.HYP_ENOMEM
+
+
+def test_a_scale_beyond_a_float_as_a_power_of_two_is_refused():
+    # 3e38 log2(e) is infinite, and a score of 0 would be 0 * infinity; where scores are capped the scale is only used over the cap
+    assert set(calls(cache(), rows(), attn._Rule(3e38, 0.0, None), OUT, TOTALS)) == {EINVAL}
+    r = attn._Rule(3e38, 50.0, None)  # its workspace is what is refused then
+    assert attn._lib().attn_token(C.byref(cache()), C.byref(r), C.byref(rows()), C.byref(OUT), C.byref(TOTALS), 4096, 0, None) == ENOMEM
