@@ -62,7 +62,7 @@ void check_rows(const hyp_attn_cache_t &c, const hyp_attn_rows_t *r, bool token)
   need(r, HYP_EINVAL, "rows is null");
   need(r->n_q_heads >= 1 && r->n_q_heads % c.n_kv_heads == 0, HYP_ESHAPE, "rows: n_q_heads must be a multiple of n_kv_heads");
   need(r->n_q_heads / c.n_kv_heads <= 256, HYP_ESHAPE, "rows: more than 256 query heads for a KV head");
-  need(r->n_rows >= 0 && r->n_rows * (r->n_q_heads / c.n_kv_heads) < (1 << 30), HYP_ESHAPE, "rows: n_rows times the group's heads must be 0..2^30 - 1");
+  need(r->n_rows >= 0 && r->n_rows <= ((1 << 30) - 1) / (r->n_q_heads / c.n_kv_heads), HYP_ESHAPE, "rows: n_rows times the group's heads must be 0..2^30 - 1");
   need(r->q || r->n_rows == 0, HYP_EINVAL, "rows: q is null");
   need(aligned(r->q, es_of(c)), HYP_EINVAL, "rows: q is not aligned to its elements");
   if (token) need(!r->q_start && r->n_rows == c.n_requests, HYP_ESHAPE, "rows: one row for each request, without q_start");
