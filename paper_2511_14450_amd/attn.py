@@ -225,6 +225,8 @@ def _workspace(need: int, workspace: Optional[torch.Tensor], device) -> Tuple[Op
         if need == 0:
             return None, None, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace: need a contiguous tensor on the cache's device")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -244,7 +246,7 @@ def attn_prompt(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: torc
         rows = _rows(cache, rule, q, q_start, see_all, q_pos, q_doc)
         out, lse, o = _outputs(cache, q, out, lse)
         need = lib.attn_workspace_bytes(cache._ref, C.byref(rows), None) if workspace is None else 0
-        workspace, ptr, size = _workspace(need, workspace, q.device)
+        workspace, ptr, size = _workspace(need, workspace, cache.device)
         _check(lib.attn_prompt(cache._ref, rule._ref, C.byref(rows), C.byref(o), ptr, size, _handle(stream, cache.device)))
     return out, lse
 
@@ -260,7 +262,7 @@ def attn_token(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_pos: Optiona
         out, lse, o = _outputs(cache, q, out, lse)
         t = None if totals is None else C.byref(_totals(cache, totals, totals_out, cache.most))
         need = lib.attn_workspace_bytes(cache._ref, C.byref(rows), t) if workspace is None else 0
-        workspace, ptr, size = _workspace(need, workspace, q.device)
+        workspace, ptr, size = _workspace(need, workspace, cache.device)
         _check(lib.attn_token(cache._ref, rule._ref, C.byref(rows), C.byref(o), t, ptr, size, _handle(stream, cache.device)))
     return out, lse
 
