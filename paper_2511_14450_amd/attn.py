@@ -92,10 +92,12 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _ints(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
+def _ints(t: Optional[torch.Tensor], shape, name: str, index: int) -> Optional[int]:
+    """The address of t, or None; index: the device's."""
     if t is None:
         return None
-    _need(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape, f"{name}: need a contiguous int32 device tensor {list(shape)}")
+    if t.get_device() != index or t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: need a contiguous int32 tensor {list(shape)} on the cache's device")
     return t.data_ptr()
 
 
@@ -117,14 +119,16 @@ class AttnCache:
         _need(k.dim() == 4 and k.shape == v.shape, "k and v: need the same shape of four dimensions")
         _need(k.dtype in (torch.float32, torch.bfloat16), "k: need float32 or bfloat16")
         n, nkv, room, d = k.shape
+        self.index = index = k.get_device()
+        _need(k.is_cuda, "k: need a device tensor")
         for t, name in ((k, "k"), (v, "v"), (prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
-            _need(t is None or (t.is_cuda and t.dtype == k.dtype and (t.stride(-1) == 1 or d == 1)), f"{name}: need a device tensor of k's type, features contiguous")
+            _need(t is None or (t.get_device() == index and t.dtype == k.dtype and (t.stride(-1) == 1 or d == 1)), f"{name}: need a tensor of k's type on its device, features contiguous")
         c = _Cache()
         if page_table is not None:
             _need(page_table.dim() == 2, "page_table: need [requests, pages per request]")
             c.n_pages, c.page_keys, c.pages_per_request = n, room, page_table.shape[1]
             n, room = page_table.shape[0], page_table.shape[1] * room
-            c.page_table = _ints(page_table, tuple(page_table.shape), "page_table")
+            c.page_table = _ints(page_table, tuple(page_table.shape), "page_table", index)
         self.most = room if most is None else int(most)
         _need(self.most <= room, f"most: {self.most} keys, room for {room}")
         self.n_requests, self.n_kv_heads, self.head_dim, self.dtype, self.device = n, nkv, d, k.dtype, k.device
@@ -132,7 +136,7 @@ class AttnCache:
         c.k_page_stride, c.k_head_stride, c.k_key_stride = k.stride()[:3]
         c.v_page_stride, c.v_head_stride, c.v_key_stride = v.stride()[:3]
         c.dtype = HYP_BF16 if k.dtype == torch.bfloat16 else HYP_F32
-        c.lens = _ints(lens, (n,), "lens")
+        c.lens = _ints(lens, (n,), "lens", index)
         _need((prefix_k is None) == (prefix_v is None), "prefix_k and prefix_v go together")
         if prefix_k is not None:
             _need(prefix_k.dim() == 3 and prefix_k.shape == prefix_v.shape and (prefix_k.shape[0], prefix_k.shape[2]) == (nkv, d),
@@ -146,8 +150,8 @@ class AttnCache:
         for t, name in ((key_pos, "key_pos"), (key_doc, "key_doc")):
             if t is None:
                 continue
-            _need(t.is_cuda and t.dtype == torch.int32 and t.dim() == 3 and tuple(t.shape[:2]) == (n, nkv) and t.shape[2] >= self.most
-                  and (t.stride(2) == 1 or t.shape[2] == 1), f"{name}: need an int32 device tensor [{n}, {nkv}, >= {self.most}], keys contiguous")
+            _need(t.get_device() == index and t.dtype == torch.int32 and t.dim() == 3 and tuple(t.shape[:2]) == (n, nkv) and t.shape[2] >= self.most
+                  and (t.stride(2) == 1 or t.shape[2] == 1), f"{name}: need an int32 tensor [{n}, {nkv}, >= {self.most}] on k's device, keys contiguous")
             setattr(c, name, t.data_ptr())
             setattr(c, name + "_request_stride", t.stride(0))
             setattr(c, name + "_head_stride", t.stride(1))
@@ -162,28 +166,30 @@ class AttnRule:
         _need(slopes is None or (slopes.is_cuda and slopes.dtype == torch.float32 and slopes.dim() == 1 and slopes.is_contiguous()),
               "slopes: need a contiguous float32 device tensor [query heads]")
         self.n_q_heads = None if slopes is None else slopes.shape[0]
+        self.index = None if slopes is None else slopes.get_device()
         self._c = _Rule(float(scale), float(cap), None if slopes is None else slopes.data_ptr())
         self._ref, self._keep = C.byref(self._c), slopes
 
 
 def _rows(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start, see_all, q_pos, q_doc) -> _Rows:
-    if q.dim() != 3 or q.dtype != cache.dtype or not q.is_cuda or q.shape[2] != cache.head_dim or (q.stride(2) != 1 and q.shape[2] != 1):
-        raise ValueError(f"q: need a {cache.dtype} device tensor [rows, query heads, {cache.head_dim}], features contiguous")
+    index = cache.index
+    if q.dim() != 3 or q.dtype != cache.dtype or q.get_device() != index or q.shape[2] != cache.head_dim or (q.stride(2) != 1 and q.shape[2] != 1):
+        raise ValueError(f"q: need a {cache.dtype} tensor [rows, query heads, {cache.head_dim}] on the cache's device, features contiguous")
     rows, heads = q.shape[0], q.shape[1]
-    _need(rule.n_q_heads is None or rule.n_q_heads == heads, "slopes: need one for each query head")
+    _need(rule.n_q_heads is None or (rule.n_q_heads == heads and rule.index == index), "slopes: need one for each query head, on the cache's device")
     return _Rows(q.data_ptr() or None, q.stride(0), q.stride(1), rows, heads,
-                 None if q_start is None else _ints(q_start, (cache.n_requests + 1,), "q_start"),
-                 None if see_all is None else _ints(see_all, (cache.n_requests,), "see_all"),
-                 None if q_pos is None else _ints(q_pos, (rows,), "q_pos"),
-                 None if q_doc is None else _ints(q_doc, (rows,), "q_doc"))
+                 None if q_start is None else _ints(q_start, (cache.n_requests + 1,), "q_start", index),
+                 None if see_all is None else _ints(see_all, (cache.n_requests,), "see_all", index),
+                 None if q_pos is None else _ints(q_pos, (rows,), "q_pos", index),
+                 None if q_doc is None else _ints(q_doc, (rows,), "q_doc", index))
 
 
 def _totals(cache: AttnCache, totals: torch.Tensor, totals_out: Optional[torch.Tensor], out_keys: int) -> _Totals:
     out = totals if totals_out is None else totals_out
     for t, keys, name in ((totals, cache.most, "totals"), (out, out_keys, "totals_out")):
-        if (t.dim() != 3 or t.dtype != torch.float32 or not t.is_cuda or t.shape[0] != cache.n_requests or t.shape[1] != cache.n_kv_heads
+        if (t.dim() != 3 or t.dtype != torch.float32 or t.get_device() != cache.index or t.shape[0] != cache.n_requests or t.shape[1] != cache.n_kv_heads
                 or t.shape[2] < keys or (t.stride(2) != 1 and t.shape[2] != 1)):
-            raise ValueError(f"{name}: need a float32 device tensor [{cache.n_requests}, {cache.n_kv_heads}, >= {keys}], keys contiguous")
+            raise ValueError(f"{name}: need a float32 tensor [{cache.n_requests}, {cache.n_kv_heads}, >= {keys}] on the cache's device, keys contiguous")
     return _Totals(totals.data_ptr(), out.data_ptr(), totals.stride(0), totals.stride(1), out.stride(0), out.stride(1))
 
 
@@ -194,10 +200,10 @@ def _on(stream):
     return _HERE if stream is None else torch.cuda.stream(stream)
 
 
-def _handle(stream, device: torch.device) -> int:
-    if stream is not None:
-        return stream.cuda_stream
-    return _raw_stream(device.index)
+def _handle(stream, index: int) -> int:
+    if torch.cuda.current_device() != index:  # where the library launches; within _on(stream) the stream's
+        raise ValueError("the cache's device is not the current one, or not the stream's")
+    return _raw_stream(index) if stream is None else stream.cuda_stream
 
 
 def _slow_raw_stream(index: int) -> int:
@@ -211,12 +217,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _slow_raw_stream)
 def _outputs(cache: AttnCache, q: torch.Tensor, out, lse):
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or (out.stride(2) != 1 and out.shape[2] != 1):
-        raise ValueError("out: need a device tensor of q's shape and type, features contiguous")
+    elif out.shape != q.shape or out.dtype != q.dtype or out.get_device() != cache.index or (out.stride(2) != 1 and out.shape[2] != 1):
+        raise ValueError("out: need a tensor of q's shape and type on its device, features contiguous")
     if lse is None:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous():
-        raise ValueError("lse: need a contiguous float32 device tensor [rows, query heads]")
+    elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or lse.get_device() != cache.index or not lse.is_contiguous():
+        raise ValueError("lse: need a contiguous float32 tensor [rows, query heads] on the cache's device")
     return out, lse, _Out(out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr())
 
 
@@ -247,7 +253,7 @@ def attn_prompt(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: torc
         out, lse, o = _outputs(cache, q, out, lse)
         need = lib.attn_workspace_bytes(cache._ref, C.byref(rows), None) if workspace is None else 0
         workspace, ptr, size = _workspace(need, workspace, cache.device)
-        _check(lib.attn_prompt(cache._ref, rule._ref, C.byref(rows), C.byref(o), ptr, size, _handle(stream, cache.device)))
+        _check(lib.attn_prompt(cache._ref, rule._ref, C.byref(rows), C.byref(o), ptr, size, _handle(stream, cache.index)))
     return out, lse
 
 
@@ -263,7 +269,7 @@ def attn_token(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_pos: Optiona
         t = None if totals is None else C.byref(_totals(cache, totals, totals_out, cache.most))
         need = lib.attn_workspace_bytes(cache._ref, C.byref(rows), t) if workspace is None else 0
         workspace, ptr, size = _workspace(need, workspace, cache.device)
-        _check(lib.attn_token(cache._ref, rule._ref, C.byref(rows), C.byref(o), t, ptr, size, _handle(stream, cache.device)))
+        _check(lib.attn_token(cache._ref, rule._ref, C.byref(rows), C.byref(o), t, ptr, size, _handle(stream, cache.index)))
     return out, lse
 
 
@@ -271,11 +277,12 @@ def attn_received(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: to
                   see_all: Optional[torch.Tensor] = None, q_pos: Optional[torch.Tensor] = None, q_doc: Optional[torch.Tensor] = None,
                   totals_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Adds the weight that own keys got from each request's last rows (0: all) to totals (in place, or into totals_out); lse: attn_prompt's."""
-    rows = _rows(cache, rule, q, q_start, see_all, q_pos, q_doc)
-    if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous():
-        raise ValueError("lse: need a contiguous float32 device tensor [rows, query heads]")
-    t = _totals(cache, totals, totals_out, cache.most)
-    _check(_lib().attn_received(cache._ref, rule._ref, C.byref(rows), lse.data_ptr(), last, C.byref(t), _handle(stream, cache.device)))
+    with _on(stream):
+        rows = _rows(cache, rule, q, q_start, see_all, q_pos, q_doc)
+        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or lse.get_device() != cache.index or not lse.is_contiguous():
+            raise ValueError("lse: need a contiguous float32 tensor [rows, query heads] on the cache's device")
+        t = _totals(cache, totals, totals_out, cache.most)
+        _check(_lib().attn_received(cache._ref, rule._ref, C.byref(rows), lse.data_ptr(), last, C.byref(t), _handle(stream, cache.index)))
     return totals if totals_out is None else totals_out
 
 
@@ -286,6 +293,7 @@ def attn_evict(cache: AttnCache, totals: torch.Tensor, keep: int, sink: int = 0,
     [n, kv heads, keep] (-1: none)."""
     lib = _lib()
     _need((into is None) == (totals_out is None), "totals_out goes with into")
+    _need(into is None or into.index == cache.index, "into: need a cache on the same device")
     with _on(stream):
         if kept is None:
             kept = torch.empty((cache.n_requests, cache.n_kv_heads, max(keep, 0)), dtype=torch.int32, device=cache.device)
@@ -293,6 +301,6 @@ def attn_evict(cache: AttnCache, totals: torch.Tensor, keep: int, sink: int = 0,
         need = lib.attn_evict_workspace_bytes(cache._ref, keep) if workspace is None else 0
         workspace, ptr, size = _workspace(need, workspace, cache.device)
         _check(lib.attn_evict(cache._ref, None if into is None else into._ref, C.byref(t), keep, sink, recent,
-                              None if now is None else _ints(now, (cache.n_requests,), "now"),
-                              _ints(kept, (cache.n_requests, cache.n_kv_heads, max(keep, 0)), "kept"), ptr, size, _handle(stream, cache.device)))
+                              None if now is None else _ints(now, (cache.n_requests,), "now", cache.index),
+                              _ints(kept, (cache.n_requests, cache.n_kv_heads, max(keep, 0)), "kept", cache.index), ptr, size, _handle(stream, cache.index)))
     return kept

@@ -56,3 +56,43 @@ def test_a_workspace_that_is_no_device_memory_of_that_size_is_refused():
             attn.attn_prompt(c, rule, f32(9, 4, 64), i32(3), out=f32(9, 4, 64), lse=f32(9, 4), workspace=ws)
         with pytest.raises(ValueError, match="workspace"):
             attn.attn_evict(c, f32(2, 2, 16), 4, kept=i32(2, 2, 4), workspace=ws)
+
+
+def test_tensors_on_another_device_than_the_cache_are_refused(monkeypatch):
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(attn, "_raw_stream", lambda index: 0)
+    parts = dict(k=f32(2, 2, 16, 64), v=f32(2, 2, 16, 64), lens=i32(2), prefix_k=f32(2, 3, 64), prefix_v=f32(2, 3, 64), key_pos=i32(2, 2, 16), key_doc=i32(2, 2, 16))
+    pages = dict(k=f32(4, 2, 16, 64), v=f32(4, 2, 16, 64), lens=i32(2), page_table=i32(2, 2))
+    for given in (parts, pages):
+        attn.AttnCache(**given)
+        for name, t in given.items():
+            with pytest.raises(ValueError):
+                attn.AttnCache(**{**given, name: On(t.t, 1)})
+    cache, rule = attn.AttnCache(**parts), attn.AttnRule(0.125)
+    small = dict(out=f32(2, 4, 64), lse=f32(2, 4), totals=f32(2, 2, 16), totals_out=f32(2, 2, 16), q_pos=i32(2), q_doc=i32(2), workspace=On(torch.zeros(0, dtype=torch.uint8)))
+
+    def refused(call, *args, **kw):
+        for i, t in enumerate(args):
+            if isinstance(t, On):
+                with pytest.raises(ValueError):
+                    call(cache, *args[:i], On(t.t, 1), *args[i + 1:], **kw)
+        for name, t in kw.items():
+            if isinstance(t, On):
+                with pytest.raises(ValueError):
+                    call(cache, *args, **{**kw, name: On(t.t, 1)})
+        current[0] = 1  # all of them on the device that is not the current one
+        with pytest.raises(ValueError, match="device"):
+            call(cache, *args, **kw)
+        current[0] = 0
+
+    refused(attn.attn_token, rule, f32(2, 4, 64), **small)
+    refused(attn.attn_prompt, rule, f32(9, 4, 64), i32(3), see_all=i32(2), q_pos=i32(9), q_doc=i32(9), out=f32(9, 4, 64), lse=f32(9, 4), workspace=small["workspace"])
+    refused(attn.attn_received, rule, f32(9, 4, 64), i32(3), f32(9, 4), f32(2, 2, 16), see_all=i32(2), q_pos=i32(9), q_doc=i32(9), totals_out=f32(2, 2, 16))
+    refused(attn.attn_evict, f32(2, 2, 16), 4, now=i32(2), kept=i32(2, 2, 4), workspace=small["workspace"])
+    into = lambda index: attn.AttnCache(f32(2, 2, 8, 64, index=index), f32(2, 2, 8, 64, index=index), i32(2, index=index))  # noqa: E731
+    with pytest.raises(ValueError):
+        attn.attn_evict(cache, f32(2, 2, 16), 4, into=into(1), totals_out=f32(2, 2, 4), kept=i32(2, 2, 4), workspace=small["workspace"])
+    for slopes in (f32(4, index=1), torch.zeros(4)):
+        with pytest.raises(ValueError):
+            attn.attn_token(cache, attn.AttnRule(0.125, slopes=slopes), f32(2, 4, 64), **small)
