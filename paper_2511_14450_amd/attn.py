@@ -92,6 +92,13 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _int32(v: int, name: str) -> int:
+    """v, where it fits the C int: ctypes would cut it."""
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name}: {v} does not fit 32 bits")
+    return v
+
+
 def _ints(t: Optional[torch.Tensor], shape, name: str, index: int) -> Optional[int]:
     """The address of t, or None; index: the device's."""
     if t is None:
@@ -126,13 +133,14 @@ class AttnCache:
         c = _Cache()
         if page_table is not None:
             _need(page_table.dim() == 2, "page_table: need [requests, pages per request]")
-            c.n_pages, c.page_keys, c.pages_per_request = n, room, page_table.shape[1]
+            c.n_pages, c.page_keys, c.pages_per_request = _int32(n, "pages"), _int32(room, "page keys"), _int32(page_table.shape[1], "pages per request")
             n, room = page_table.shape[0], page_table.shape[1] * room
             c.page_table = _ints(page_table, tuple(page_table.shape), "page_table", index)
-        self.most = room if most is None else int(most)
+        self.most = _int32(room if most is None else int(most), "most")
         _need(self.most <= room, f"most: {self.most} keys, room for {room}")
         self.n_requests, self.n_kv_heads, self.head_dim, self.dtype, self.device = n, nkv, d, k.dtype, k.device
-        c.k, c.v, c.most, c.n_requests, c.n_kv_heads, c.head_dim = k.data_ptr(), v.data_ptr(), self.most, n, nkv, d
+        c.k, c.v, c.most = k.data_ptr(), v.data_ptr(), self.most
+        c.n_requests, c.n_kv_heads, c.head_dim = _int32(n, "requests"), _int32(nkv, "heads"), _int32(d, "features")
         c.k_page_stride, c.k_head_stride, c.k_key_stride = k.stride()[:3]
         c.v_page_stride, c.v_head_stride, c.v_key_stride = v.stride()[:3]
         c.dtype = HYP_BF16 if k.dtype == torch.bfloat16 else HYP_F32
@@ -141,7 +149,7 @@ class AttnCache:
         if prefix_k is not None:
             _need(prefix_k.dim() == 3 and prefix_k.shape == prefix_v.shape and (prefix_k.shape[0], prefix_k.shape[2]) == (nkv, d),
                   f"prefix_k and prefix_v: need [{nkv}, keys, {d}]")
-            c.prefix_len = prefix_k.shape[1]
+            c.prefix_len = _int32(prefix_k.shape[1], "prefix")
             if c.prefix_len:
                 c.prefix_k, c.prefix_v = prefix_k.data_ptr(), prefix_v.data_ptr()
             c.prefix_k_head_stride, c.prefix_k_key_stride = prefix_k.stride()[:2]
@@ -177,7 +185,7 @@ def _rows(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start, see_all, q
         raise ValueError(f"q: need a {cache.dtype} tensor [rows, query heads, {cache.head_dim}] on the cache's device, features contiguous")
     rows, heads = q.shape[0], q.shape[1]
     _need(rule.n_q_heads is None or (rule.n_q_heads == heads and rule.index == index), "slopes: need one for each query head, on the cache's device")
-    return _Rows(q.data_ptr() or None, q.stride(0), q.stride(1), rows, heads,
+    return _Rows(q.data_ptr() or None, q.stride(0), q.stride(1), rows, _int32(heads, "query heads"),
                  None if q_start is None else _ints(q_start, (cache.n_requests + 1,), "q_start", index),
                  None if see_all is None else _ints(see_all, (cache.n_requests,), "see_all", index),
                  None if q_pos is None else _ints(q_pos, (rows,), "q_pos", index),
@@ -282,7 +290,7 @@ def attn_received(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: to
         if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or lse.get_device() != cache.index or not lse.is_contiguous():
             raise ValueError("lse: need a contiguous float32 tensor [rows, query heads] on the cache's device")
         t = _totals(cache, totals, totals_out, cache.most)
-        _check(_lib().attn_received(cache._ref, rule._ref, C.byref(rows), lse.data_ptr(), last, C.byref(t), _handle(stream, cache.index)))
+        _check(_lib().attn_received(cache._ref, rule._ref, C.byref(rows), lse.data_ptr(), _int32(last, "last"), C.byref(t), _handle(stream, cache.index)))
     return totals if totals_out is None else totals_out
 
 
@@ -292,6 +300,8 @@ def attn_evict(cache: AttnCache, totals: torch.Tensor, keep: int, sink: int = 0,
     """Keeps at most `keep` keys of every request and KV head, in place or into another cache; returns the slots they came from
     [n, kv heads, keep] (-1: none)."""
     lib = _lib()
+    for value, name in ((keep, "keep"), (sink, "sink"), (recent, "recent")):
+        _int32(value, name)
     _need((into is None) == (totals_out is None), "totals_out goes with into")
     _need(into is None or into.index == cache.index, "into: need a cache on the same device")
     with _on(stream):

@@ -96,3 +96,8 @@ def test_tensors_on_another_device_than_the_cache_are_refused(monkeypatch):
     for slopes in (f32(4, index=1), torch.zeros(4)):
         with pytest.raises(ValueError):
             attn.attn_token(cache, attn.AttnRule(0.125, slopes=slopes), f32(2, 4, 64), **small)
+
+
+def test_a_number_of_kept_keys_beyond_32_bits_is_refused():
+    with pytest.raises(ValueError, match="keep"):
+        attn.attn_evict(attn.AttnCache(f32(1, 1, 8, 64), f32(1, 1, 8, 64), i32(1)), f32(1, 1, 8), (1 << 32) + 4)
