@@ -144,8 +144,9 @@ HYP_API hyp_status_t attn_received(const hyp_attn_cache_t *cache, const hyp_attn
  *   now    [n_requests] or null
  *   kept   [n_requests][n_kv_heads][keep]: the slot each key came from, -1 behind the last one
  *   workspace  >= attn_evict_workspace_bytes(), 16-byte aligned
- * HYP_EINVAL also: keep < 1, sink or recent < 0, sink + recent > keep, totals of key_pos / key_doc
- * that all heads share moved in place. */
+ * HYP_EINVAL also: keep < 1, sink or recent < 0, sink + recent > keep, a result whose requests or
+ * heads share keys, values, key_pos, key_doc or totals (a stride of 0).  Pages that several
+ * requests' tables name are the caller's to keep out of an eviction in place, and of `into`. */
 HYP_API size_t attn_evict_workspace_bytes(const hyp_attn_cache_t *cache, int32_t keep);
 HYP_API hyp_status_t attn_evict(const hyp_attn_cache_t *cache, const hyp_attn_cache_t *into, const hyp_attn_totals_t *totals,
                                 int32_t keep, int32_t sink, int32_t recent, const int32_t *now, int32_t *kept,

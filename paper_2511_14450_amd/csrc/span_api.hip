@@ -23,6 +23,8 @@ inline void need(bool ok, hyp_status_t status, const char *text) {
 
 int es_of(const hyp_attn_cache_t &c) { return c.dtype == HYP_BF16 ? 2 : 4; }
 
+bool apart(int64_t stride, int64_t n) { return n <= 1 || stride != 0; }
+
 bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
 
 int shift_of(const hyp_attn_cache_t &c) {
@@ -342,8 +344,17 @@ hyp_status_t attn_evict(const hyp_attn_cache_t *cache, const hyp_attn_cache_t *i
     } else {
       need(totals->in == totals->out, HYP_EINVAL, "totals: in place means out == in");
     }
-    need(cache->n_kv_heads == 1 || ((!p.to.key_pos || p.to.key_pos_head_stride != 0) && (!p.to.key_doc || p.to.key_doc_head_stride != 0)), HYP_EINVAL,
-         "key_pos or key_doc of the result are shared by its heads, which keep different keys");
+    need(!into || ((!into->key_pos || into->key_pos != cache->key_pos) && (!into->key_doc || into->key_doc != cache->key_doc)), HYP_EINVAL,
+         "into: shares key_pos or key_doc with the cache");
+    // requests and heads keep different keys: what the result shares would be written by several workgroups, in place while others read it
+    const hyp_attn_cache_t &to = p.to;
+    const int64_t n = to.n_requests, heads = to.n_kv_heads, slabs = to.page_table ? to.n_pages : n, keys = to.page_table ? to.page_keys : to.most;
+    need(apart(to.k_page_stride, slabs) && apart(to.k_head_stride, heads) && apart(to.k_key_stride, keys) && apart(to.v_page_stride, slabs) &&
+             apart(to.v_head_stride, heads) && apart(to.v_key_stride, keys), HYP_EINVAL, "k or v of the result are shared by its requests, heads or keys");
+    need((!to.key_pos || (apart(to.key_pos_request_stride, n) && apart(to.key_pos_head_stride, heads))) &&
+             (!to.key_doc || (apart(to.key_doc_request_stride, n) && apart(to.key_doc_head_stride, heads))), HYP_EINVAL,
+         "key_pos or key_doc of the result are shared by its requests or heads");
+    need(apart(totals->out_request_stride, n) && apart(totals->out_head_stride, heads), HYP_EINVAL, "totals of the result are shared by its requests or heads");
     const size_t bytes = (size_t)cache->n_requests * cache->n_kv_heads * 2 * keep * 4;
     need(workspace && aligned(workspace, 16), HYP_EINVAL, "workspace is null or not aligned to 16 bytes");
     need(workspace_bytes >= bytes, HYP_ENOMEM, "workspace is smaller than attn_evict_workspace_bytes()");

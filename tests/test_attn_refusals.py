@@ -101,3 +101,23 @@ def test_tensors_on_another_device_than_the_cache_are_refused(monkeypatch):
 def test_a_number_of_kept_keys_beyond_32_bits_is_refused():
     with pytest.raises(ValueError, match="keep"):
         attn.attn_evict(attn.AttnCache(f32(1, 1, 8, 64), f32(1, 1, 8, 64), i32(1)), f32(1, 1, 8), (1 << 32) + 4)
+
+
+MOVES = dict(key_pos=4096, key_pos_request_stride=32, key_pos_head_stride=16, key_doc=8192, key_doc_request_stride=32, key_doc_head_stride=16)
+
+
+@pytest.mark.parametrize("shared", ["key_pos_request_stride", "key_doc_request_stride", "key_pos_head_stride", "key_doc_head_stride", "k_page_stride", "v_page_stride",
+                                    "k_head_stride", "v_head_stride", "k_key_stride", "v_key_stride"])
+def test_evictions_to_memory_that_requests_or_heads_share_are_refused(shared):
+    lib, more = attn._lib(), {**MOVES, shared: 0}
+    c, into = cache(**more), cache(**{**more, "k": 64, "v": 128, "lens": 64})
+    assert lib.attn_evict(C.byref(c), None, C.byref(TOTALS), 4, 0, 0, None, 4096, 4096, 1 << 20, None) == EINVAL
+    apart = attn._Totals(4096, 8192, 32, 16, 32, 16)
+    source = cache(key_pos=1 << 20, key_doc=1 << 20)  # a source that is only read may share
+    assert lib.attn_evict(C.byref(source), C.byref(into), C.byref(apart), 4, 0, 0, None, 4096, 4096, 1 << 20, None) == EINVAL
+    # as are evictions to the source's own positions or ids, and totals that requests or heads share
+    for same in (dict(key_pos=4096, key_pos_request_stride=32, key_pos_head_stride=16), dict(key_doc=4096, key_doc_request_stride=32, key_doc_head_stride=16)):
+        c, into = cache(**same), cache(**{**same, "k": 64, "v": 128, "lens": 64})
+        assert lib.attn_evict(C.byref(c), C.byref(into), C.byref(apart), 4, 0, 0, None, 4096, 4096, 1 << 20, None) == EINVAL
+    for flat in (attn._Totals(4096, 4096, 0, 16, 0, 16), attn._Totals(4096, 4096, 32, 0, 32, 0)):
+        assert lib.attn_evict(C.byref(cache()), None, C.byref(flat), 4, 0, 0, None, 4096, 4096, 1 << 20, None) == EINVAL
