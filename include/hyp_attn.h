@@ -111,7 +111,8 @@ HYP_API size_t attn_workspace_bytes(const hyp_attn_cache_t *cache, const hyp_att
 
 /* out and lse of all rows.  workspace: >= attn_workspace_bytes(cache, rows, null), 16-byte aligned;
  * one call at a time may use it.
- * Errors of all calls: HYP_EINVAL (null pointer, bad enum or value, workspace misaligned),
+ * Errors of all calls: HYP_EINVAL (null pointer, bad enum or value, workspace misaligned, results
+ * that share memory by a stride of 0),
  * HYP_ESHAPE (sizes that do not go together), HYP_ENOMEM (workspace too small), HYP_EDEVICE. */
 HYP_API hyp_status_t attn_prompt(const hyp_attn_cache_t *cache, const hyp_attn_rule_t *rule, const hyp_attn_rows_t *rows,
                                  const hyp_attn_out_t *out, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -76,6 +76,9 @@ void check_totals(const hyp_attn_totals_t *t) {
   need(t->in != t->out || (t->in_request_stride == t->out_request_stride && t->in_head_stride == t->out_head_stride), HYP_EINVAL,
        "totals: in place with unequal strides");
 }
+void check_apart(const hyp_attn_cache_t &c, const hyp_attn_totals_t &t) {
+  need(apart(t.out_request_stride, c.n_requests) && apart(t.out_head_stride, c.n_kv_heads), HYP_EINVAL, "totals: requests or heads share those that are written");
+}
 
 // Rows of keys and queries can be fetched in aligned 16-byte pieces, and a stage's rows lie within 31 bits of its first
 bool is_wide(const hyp_attn_cache_t &c, const hyp_attn_rows_t &r) {
@@ -132,6 +135,7 @@ void add_out(SpanCall &p, const hyp_attn_out_t *o) {
   need(o && (o->out || p.n_rows == 0), HYP_EINVAL, "out is null");
   const int es = es_of(p.c);
   need(aligned(o->out, es), HYP_EINVAL, "out is not aligned to its elements");
+  need(p.n_rows == 0 || (apart(o->out_row_stride, p.n_rows) && apart(o->out_head_stride, p.nq)), HYP_EINVAL, "out: rows or heads share their results");
   p.out = o->out;
   p.out_rs = o->out_row_stride;
   p.out_hs = o->out_head_stride;
@@ -272,7 +276,10 @@ hyp_status_t attn_token(const hyp_attn_cache_t *cache, const hyp_attn_rule_t *ru
     check_cache(cache);
     check_rule(rule);
     check_rows(*cache, rows, true);
-    if (totals) check_totals(totals);
+    if (totals) {
+      check_totals(totals);
+      check_apart(*cache, *totals);
+    }
     SpanCall p = begin(*cache, *rows);
     add_rule(p, *rule);
     add_out(p, out);
@@ -292,6 +299,7 @@ hyp_status_t attn_received(const hyp_attn_cache_t *cache, const hyp_attn_rule_t 
     check_rule(rule);
     check_rows(*cache, rows, false);
     check_totals(totals);
+    check_apart(*cache, *totals);
     need(lse || rows->n_rows == 0, HYP_EINVAL, "lse is null");
     need(last >= 0, HYP_EINVAL, "last is negative");
     SpanCall p = begin(*cache, *rows);
@@ -354,7 +362,7 @@ hyp_status_t attn_evict(const hyp_attn_cache_t *cache, const hyp_attn_cache_t *i
     need((!to.key_pos || (apart(to.key_pos_request_stride, n) && apart(to.key_pos_head_stride, heads))) &&
              (!to.key_doc || (apart(to.key_doc_request_stride, n) && apart(to.key_doc_head_stride, heads))), HYP_EINVAL,
          "key_pos or key_doc of the result are shared by its requests or heads");
-    need(apart(totals->out_request_stride, n) && apart(totals->out_head_stride, heads), HYP_EINVAL, "totals of the result are shared by its requests or heads");
+    check_apart(*cache, *totals);
     const size_t bytes = (size_t)cache->n_requests * cache->n_kv_heads * 2 * keep * 4;
     need(workspace && aligned(workspace, 16), HYP_EINVAL, "workspace is null or not aligned to 16 bytes");
     need(workspace_bytes >= bytes, HYP_ENOMEM, "workspace is smaller than attn_evict_workspace_bytes()");

@@ -121,3 +121,21 @@ def test_evictions_to_memory_that_requests_or_heads_share_are_refused(shared):
         assert lib.attn_evict(C.byref(c), C.byref(into), C.byref(apart), 4, 0, 0, None, 4096, 4096, 1 << 20, None) == EINVAL
     for flat in (attn._Totals(4096, 4096, 0, 16, 0, 16), attn._Totals(4096, 4096, 32, 0, 32, 0)):
         assert lib.attn_evict(C.byref(cache()), None, C.byref(flat), 4, 0, 0, None, 4096, 4096, 1 << 20, None) == EINVAL
+
+
+@pytest.mark.parametrize("strides", [(0, 64), (256, 0)])
+def test_outputs_that_rows_or_heads_share_are_refused(strides):
+    lib, out = attn._lib(), attn._Out(4096, *strides, 4096)
+    prompt = rows(q_start=4096)
+    assert lib.attn_prompt(C.byref(cache()), C.byref(attn._Rule(1.0, 0.0, None)), C.byref(prompt), C.byref(out), 4096, 1 << 30, None) == EINVAL
+    assert lib.attn_token(C.byref(cache()), C.byref(attn._Rule(1.0, 0.0, None)), C.byref(rows()), C.byref(out), None, 4096, 1 << 30, None) == EINVAL
+    none = rows(q_start=4096, n_rows=0, q=None)  # no rows, nothing shared
+    assert lib.attn_prompt(C.byref(cache()), C.byref(attn._Rule(1.0, 0.0, None)), C.byref(none), C.byref(attn._Out()), None, 0, None) == binding.HYP_OK
+
+
+@pytest.mark.parametrize("strides", [(0, 16), (32, 0)])
+def test_totals_that_requests_or_heads_share_are_refused(strides):
+    lib, prompt, rule = attn._lib(), rows(q_start=4096), attn._Rule(1.0, 0.0, None)
+    for totals in (attn._Totals(4096, 4096, *strides, *strides), attn._Totals(4096, 8192, 32, 16, *strides)):
+        assert lib.attn_received(C.byref(cache()), C.byref(rule), C.byref(prompt), 4096, 0, C.byref(totals), None) == EINVAL
+        assert lib.attn_token(C.byref(cache()), C.byref(rule), C.byref(rows()), C.byref(OUT), C.byref(totals), 4096, 1 << 30, None) == EINVAL
