@@ -23,6 +23,9 @@ inline void need(bool ok, hyp_status_t status, const char *text) {
 
 int es_of(const hyp_attn_cache_t &c) { return c.dtype == HYP_BF16 ? 2 : 4; }
 
+// A launch has fewer than 2^32 lanes; one that is refused would leave the launches after it without what it writes.
+void check_launch(int64_t workgroups, int threads) { need(workgroups < (1ll << 32) / threads, HYP_ESHAPE, "too much work for a launch"); }
+
 bool apart(int64_t stride, int64_t n) { return n <= 1 || stride != 0; }
 
 bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
@@ -157,9 +160,10 @@ Plan plan_prompt(SpanCall &p, bool wide) {
   const int64_t stages = (p.c.prefix_len + stage - 1) / stage + (p.c.most + stage - 1) / stage;
   p.tiles = (int)tiles;
   p.splits = span_prompt_splits(tiles * p.c.n_kv_heads, stages, es == 2 ? 4 : 2);
-  need(tiles * p.splits * (p.c.n_kv_heads + 8) < (1ll << 31), HYP_ESHAPE, "too many row tiles for a launch");
+  check_launch(span_head_items(p.c.n_kv_heads, tiles * p.splits), 64 * kSpanWaves);
   Plan w;
   if (p.splits > 1) {
+    check_launch((p.n_rows * p.nq + 3) / 4, 256);
     w.part_o = (p.splits * p.n_rows * p.nq * p.c.head_dim + 3) / 4 * 4;  // pairs of floats follow
     w.part_ml = (int64_t)p.splits * p.n_rows * p.nq * 2;
   }
@@ -175,11 +179,12 @@ Plan plan_token(SpanCall &p, bool wide, bool totals) {
   p.pre_tiles = t.pre_tiles;
   p.pre_splits = t.pre_splits;
   const int64_t pre = (int64_t)t.pre_tiles * t.pre_splits * p.c.n_kv_heads, own = (int64_t)p.c.n_requests * t.tiles * t.splits * p.c.n_kv_heads;
-  need(pre + own < (1ll << 31), HYP_ESHAPE, "too many items for a launch");
+  check_launch(pre + own, 64 * span_token_waves(nt, es));
   p.pre_items = (int)pre;
   Plan w;
   const int64_t slots = t.splits + t.pre_splits;
   if (slots > 1 || totals) {
+    check_launch((p.n_rows * p.nq + 3) / 4 + (totals ? (int64_t)((p.c.most + 1023) / 1024) * p.c.n_kv_heads * p.c.n_requests : 0), 256);
     w.part_o = slots * p.n_rows * p.nq * p.c.head_dim;
     w.part_ml = slots * p.n_rows * p.nq * 2;
   }
@@ -313,8 +318,8 @@ hyp_status_t attn_received(const hyp_attn_cache_t *cache, const hyp_attn_rule_t 
     // 150 instead of 119), nor where the pairs do not fill the chip (one prompt of 3500 rows, 140 of them: 276 instead of 263; 2048, 80: 183, 165).
     const int64_t counts = last ? std::min(last, p.c.most) : p.c.most, pairs = (int64_t)((p.c.most + 255) / 256) * p.c.n_requests * p.c.n_kv_heads;
     p.pairs_of_blocks = 2 * counts > p.c.most && counts * p.G > 512 && pairs >= 160;
-    const int64_t blocks = (int64_t)((p.c.most + 63) / 64) * p.c.n_requests * (p.c.n_kv_heads + 8);
-    need(blocks < (1ll << 31), HYP_ESHAPE, "too many keys for a launch");
+    const SpanReceived form = span_received_form(span_steps(p.c.head_dim, wide), es_of(p.c), p.pairs_of_blocks);
+    check_launch(span_head_items(p.c.n_kv_heads, span_received_items(p, form.keys)), 64 * form.waves);
     const hipStream_t s = (hipStream_t)hip_stream;
     run(p.c.dtype == HYP_BF16 ? span_received<bf16_t>(p, wide, s) : span_received<float>(p, wide, s));
   });
@@ -366,7 +371,6 @@ hyp_status_t attn_evict(const hyp_attn_cache_t *cache, const hyp_attn_cache_t *i
     const size_t bytes = (size_t)cache->n_requests * cache->n_kv_heads * 2 * keep * 4;
     need(workspace && aligned(workspace, 16), HYP_EINVAL, "workspace is null or not aligned to 16 bytes");
     need(workspace_bytes >= bytes, HYP_ENOMEM, "workspace is smaller than attn_evict_workspace_bytes()");
-    need((int64_t)cache->n_requests * cache->n_kv_heads * ((keep + 31) / 32) < (1ll << 31), HYP_ESHAPE, "too many slots for a launch");
     p.page_shift = shift_of(p.c);
     p.to_page_shift = shift_of(p.to);
     p.totals = *totals;
@@ -382,6 +386,13 @@ hyp_status_t attn_evict(const hyp_attn_cache_t *cache, const hyp_attn_cache_t *i
              c.k_key_stride % per == 0 && c.v_page_stride % per == 0 && c.v_head_stride % per == 0 && c.v_key_stride % per == 0;
     };
     p.vec = wide(p.c) && wide(p.to);
+    const int64_t pairs = (int64_t)p.c.n_requests * p.c.n_kv_heads;
+    if (span_evict_once(p)) {
+      check_launch(pairs, kEvictSmall);
+    } else {
+      check_launch(pairs, kEvictThreads);
+      check_launch(pairs * ((keep + kEvictRows - 1) / kEvictRows), 256);
+    }
     run(span_evict(p, (hipStream_t)hip_stream));
   });
 }

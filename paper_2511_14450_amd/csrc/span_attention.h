@@ -550,8 +550,6 @@ template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> __global__ vo
   if (p.pairs_of_blocks && blocks - 1 - i > i) r.block((blocks - 1 - i) * R::KEYS, in, out);
 }
 
-inline unsigned head_items(int heads, int items) { return 8u * ((unsigned)(heads >> 3) * items + ((unsigned)(heads & 7) * items + 7) / 8); }
-
 // most: LDS that any call of the kernel asks for; told to the device once
 template <auto K> hipError_t span_launch(int lds, int most, unsigned blocks, int threads, const SpanCall &p, hipStream_t s) {
   static std::atomic<uint64_t> told{0};  // by device
@@ -589,7 +587,7 @@ template <typename T> hipError_t span_prompt(const SpanCall &p, bool wide, hipSt
     constexpr bool W = decltype(w)::value;
     using S = Span<T, NT, kSpanWaves, 1, span_stage_keys(NT, sizeof(T)), 2, W>;
     return span_launch<k_span_prompt<T, NT, W>>(S::LDS_ALL + (p.c.key_doc ? Survey<S>::LDS : 0), S::LDS_ALL + Survey<S>::LDS,
-                                                head_items(p.c.n_kv_heads, p.tiles * p.splits), 64 * kSpanWaves, p, s);
+                                                (unsigned)span_head_items(p.c.n_kv_heads, p.tiles * p.splits), 64 * kSpanWaves, p, s);
   });
 }
 
@@ -609,19 +607,15 @@ template <typename T> hipError_t span_received(const SpanCall &p, bool wide, hip
   return span_pick(p.c.head_dim, wide, [&](auto nt, auto w) {
     constexpr int NT = decltype(nt)::value;
     constexpr bool W = decltype(w)::value;
-    constexpr int CPR = span_chunks(NT, sizeof(T));
     SpanCall call = p;
-    auto go = [&](auto rows, auto kb, auto nw) {
-      constexpr int ROWS = decltype(rows)::value, KB = decltype(kb)::value, NW = decltype(nw)::value;
-      using R = Received<T, NT, W, ROWS, KB, NW>;
-      const int blocks = (p.c.most + R::KEYS - 1) / R::KEYS, items = p.pairs_of_blocks ? (blocks + 1) / 2 : blocks;
-      call.one_stage = p.last > 0 && (int64_t)p.last * p.G <= ROWS;
-      return span_launch<k_span_received<T, NT, W, ROWS, KB, NW>>(call.one_stage ? R::LDS_ONE : R::LDS, R::LDS, head_items(p.c.n_kv_heads, items * p.c.n_requests), 64 * NW, call, s);
+    auto go = [&](auto pairs) {
+      constexpr SpanReceived F = span_received_form(NT, sizeof(T), decltype(pairs)::value);
+      using R = Received<T, NT, W, F.rows, F.keys / 64, F.waves>;
+      call.one_stage = p.last > 0 && (int64_t)p.last * p.G <= F.rows;
+      return span_launch<k_span_received<T, NT, W, F.rows, F.keys / 64, F.waves>>(call.one_stage ? R::LDS_ONE : R::LDS, R::LDS,
+                                                                                 (unsigned)span_head_items(p.c.n_kv_heads, span_received_items(p, F.keys)), 64 * F.waves, call, s);
     };
-    using std::integral_constant;
-    constexpr int few = CPR <= 32 ? 128 : 64;  // rows of a stage that fit LDS twice
-    if (!p.pairs_of_blocks) return go(integral_constant<int, few>(), integral_constant<int, 1>(), integral_constant<int, 4>());
-    return go(integral_constant<int, few>(), integral_constant<int, CPR <= 16 ? 2 : 1>(), integral_constant<int, few / 16>());
+    return p.pairs_of_blocks ? go(std::true_type()) : go(std::false_type());
   });
 }
 

@@ -4,7 +4,7 @@
 namespace hyp {
 namespace {
 
-constexpr int kSelectThreads = 1024, kMoveRows = 32;
+constexpr int kSelectThreads = kEvictThreads, kMoveRows = kEvictRows;
 
 typedef __attribute__((__vector_size__(16))) float f32x4_t;
 
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
 
 // The same for up to 256 keys, and their move, in one launch: a key stays if fewer than `keep` come before it, counted one by one.  Latency
 // bounds it, 8 us for caches of 96 keys.  A call takes 13 us for 96 keys, 17 for 256; in two launches 17 for either, and for 512 (25 in one).
-constexpr int kSmall = 256;
+constexpr int kSmall = kEvictSmall;
 template <bool VEC, int ES> __device__ void move_rows(const EvictCall &p, int b, int kvh, int r0, int rows, const int *kept, int threads);
 
 template <bool VEC, int ES> __global__ void __launch_bounds__(kSmall) k_evict_small(const EvictCall p) {
@@ -276,12 +276,13 @@ template <bool VEC, int ES> __device__ void move_rows(const EvictCall &p, int b,
 
 template <bool VEC, int ES> static hipError_t evict(const EvictCall &p, hipStream_t s) {
   const unsigned pairs = (unsigned)p.c.n_requests * p.c.n_kv_heads;
-  // In place the new lengths may be written only after all heads' workgroups have read the old ones: two launches.
-  if (!p.in_place && p.c.most <= kSmall) {
+  if (span_evict_once(p)) {
     k_evict_small<VEC, ES><<<pairs, kSmall, 0, s>>>(p);
     return hipGetLastError();
   }
   k_evict_select<<<pairs, kSelectThreads, 0, s>>>(p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;  // the move goes by what the selection wrote
   k_evict_move<VEC, ES><<<pairs * ((p.keep + kMoveRows - 1) / kMoveRows), 256, 0, s>>>(p);
   return hipGetLastError();
 }

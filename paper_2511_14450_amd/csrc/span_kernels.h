@@ -67,4 +67,24 @@ __host__ __device__ constexpr int span_steps_waves(int nt) { return nt <= 8 ? 2 
 constexpr int kSpanWaves = 4;          // attn_prompt: waves of 32 rows
 constexpr int kSpanTile = 32 * kSpanWaves;
 
+
+// Workgroups of a launch over `items` of each of the KV heads, which go to the eight XCDs in turn (head_item).
+constexpr int64_t span_head_items(int64_t heads, int64_t items) { return 8 * ((heads >> 3) * items + ((heads & 7) * items + 7) / 8); }
+
+// attn_received: rows of a stage that fit LDS twice, keys of a block (64, or 128 where two fit the registers), waves.
+struct SpanReceived { int rows, keys, waves; };
+constexpr SpanReceived span_received_form(int nt, int es, bool pairs_of_blocks) {
+  const int rows = span_chunks(nt, es) <= 32 ? 128 : 64;
+  return {rows, pairs_of_blocks && span_chunks(nt, es) <= 16 ? 128 : 64, pairs_of_blocks ? rows / 16 : 4};
+}
+inline int64_t span_received_items(const SpanCall &p, int keys) {  // of a KV head
+  const int64_t blocks = (p.c.most + keys - 1) / keys;
+  return (p.pairs_of_blocks ? (blocks + 1) / 2 : blocks) * p.c.n_requests;
+}
+
+// attn_evict: in one launch up to so many keys, else by so many threads, and moved so many slots at a time.
+constexpr int kEvictSmall = 256, kEvictThreads = 1024, kEvictRows = 32;
+// In place the new lengths may be written only after all heads' workgroups have read the old ones: two launches.
+inline bool span_evict_once(const EvictCall &p) { return !p.in_place && p.c.most <= kEvictSmall; }
+
 }  // namespace hyp

@@ -139,3 +139,24 @@ def test_totals_that_requests_or_heads_share_are_refused(strides):
     for totals in (attn._Totals(4096, 4096, *strides, *strides), attn._Totals(4096, 8192, 32, 16, *strides)):
         assert lib.attn_received(C.byref(cache()), C.byref(rule), C.byref(prompt), 4096, 0, C.byref(totals), None) == EINVAL
         assert lib.attn_token(C.byref(cache()), C.byref(rule), C.byref(rows()), C.byref(OUT), C.byref(totals), 4096, 1 << 30, None) == EINVAL
+
+
+def test_calls_beyond_a_launch_are_refused():
+    # a launch has fewer than 2^32 lanes: 2^22 workgroups of 1024 are too many, and so are 2^24 of 256
+    lib, evict = attn._lib(), dict(n_requests=1 << 22, n_kv_heads=1)
+    for into in (None, C.byref(cache(**evict, k=64, v=128, lens=64, most=300))):
+        totals = attn._Totals(4096, 4096, 32, 16, 32, 16) if into is None else attn._Totals(4096, 8192, 32, 16, 32, 16)
+        assert lib.attn_evict(C.byref(cache(**evict, most=300)), into, C.byref(totals), 4, 0, 0, None, 4096, 4096, 1 << 40, None) == ESHAPE
+    many = cache(n_requests=(1 << 22) - 1, n_kv_heads=1, most=129)
+    assert lib.attn_evict(C.byref(many), None, C.byref(TOTALS), 129, 0, 0, None, 4096, 4096, 1 << 40, None) == ESHAPE  # five workgroups of 256 a request move
+    rule = attn._Rule(1.0, 0.0, None)
+    wide = cache(n_requests=(1 << 24) - 1, n_kv_heads=1, head_dim=8)
+    one = attn._Rows(q=4096, q_row_stride=256, q_head_stride=64, n_rows=(1 << 24) - 1, n_q_heads=2)
+    totals = attn._Totals(4096, 4096, 32, 16, 32, 16)
+    assert lib.attn_token(C.byref(wide), C.byref(rule), C.byref(one), C.byref(OUT), C.byref(totals), 4096, 1 << 50, None) == ESHAPE  # the join's
+    one.q_start = 4096
+    received = cache(n_requests=(1 << 24) - 1, n_kv_heads=1, head_dim=8, most=65)
+    assert lib.attn_received(C.byref(received), C.byref(rule), C.byref(one), 4096, 0, C.byref(totals), None) == ESHAPE
+    long = attn._Rows(q=4096, q_row_stride=256, q_head_stride=8, n_rows=1 << 21, n_q_heads=1 << 10, q_start=4096)
+    heads = cache(n_requests=1, n_kv_heads=1 << 10, head_dim=8)
+    assert lib.attn_prompt(C.byref(heads), C.byref(rule), C.byref(long), C.byref(OUT), 4096, 1 << 50, None) == ESHAPE
