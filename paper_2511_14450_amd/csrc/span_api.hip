@@ -313,11 +313,7 @@ hyp_status_t attn_received(const hyp_attn_cache_t *cache, const hyp_attn_rule_t 
     p.lse_in = lse;
     p.last = last;
     const bool wide = is_wide(*cache, *rows);
-    // Causality gives the first keys the most rows, and pairs of blocks even that out, of 128 keys, which fetch the rows half as often: 8 prompts of
-    // 2048 rows of 32 heads 290 instead of 350 us, one of 4500 of 40 heads 337 instead of 399.  Not where all blocks meet as many rows (the last 512:
-    // 150 instead of 119), nor where the pairs do not fill the chip (one prompt of 3500 rows, 140 of them: 276 instead of 263; 2048, 80: 183, 165).
-    const int64_t counts = last ? std::min(last, p.c.most) : p.c.most, pairs = (int64_t)((p.c.most + 255) / 256) * p.c.n_requests * p.c.n_kv_heads;
-    p.pairs_of_blocks = 2 * counts > p.c.most && counts * p.G > 512 && pairs >= 160;
+    p.pairs_of_blocks = span_received_pairs(p.c.most, last, p.c.n_requests, p.c.n_kv_heads, p.G);
     const SpanReceived form = span_received_form(span_steps(p.c.head_dim, wide), es_of(p.c), p.pairs_of_blocks);
     check_launch(span_head_items(p.c.n_kv_heads, span_received_items(p, form.keys)), 64 * form.waves);
     const hipStream_t s = (hipStream_t)hip_stream;

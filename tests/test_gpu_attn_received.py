@@ -1,11 +1,13 @@
-"""The weight that keys receive (attn_received): how exactly the rows' log-sum-exps count."""
+"""The weight that keys receive (attn_received): how exactly the rows' log-sum-exps count, and the form that calls of many keys take, over the layouts,
+rules and masks that the other form's tests have."""
 import math
 
 import pytest
 import torch
 
 import paper_2511_14450_amd as hyp
-from tests.test_gpu_attn import BF, F32
+from tests import attn_received_cases as cases
+from tests.test_gpu_attn import BF, F32, Problem, check_prompt
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +33,21 @@ def test_a_log_sum_exp_counts_in_full(dtype, rule, held, rows):
         want = torch.tensor([exact * sum(j <= held - rows + i for i in range(rows)) for j in range(held)], dtype=torch.float64)
         worst = max(worst, float(((got[0, 0].double().cpu() - want) / want).abs().max()))
     assert worst <= 2.0 ** -22 + 2.0 ** -40 + 2 * 2.0 ** -23, worst
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("case", cases.ALL, ids=cases.name)
+def test_pairs_of_blocks(dtype, case):
+    check_prompt(cases.problem(case, dtype, Problem), last=case["last"])
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("d", [128, 33])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_pairs_of_blocks_with_numbers_that_a_row_does_not_see(dtype, d, bad):
+    # keys of an id that no row has, beside the others; and behind the requests' last keys, as always
+    pr = cases.problem(cases.case(d=d, rule=dict(docs=3)), dtype, Problem)
+    pr.q_doc.clamp_(0, 2)
+    pr.key_doc[:, :, 7] = pr.key_doc[:, :, 130] = 99
+    pr.k[:, :, 7] = pr.k[:, :, 130] = bad
+    check_prompt(pr)
