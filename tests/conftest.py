@@ -13,6 +13,9 @@ def pytest_configure(config):
 
 
 def pytest_collection_modifyitems(config, items):
+    # Whether a burst of tasks finds a node busy depends on how fast the host and the device are, and one test asks for it: it
+    # runs last, so that its failure under -x leaves no other test unrun.  test_tier_host.py and test_gpu_tier_held.py hold the tasks.
+    items.sort(key=lambda it: "test_any_node_gives_the_lone_stage_result" in it.nodeid)
     # Tests marked gpu are skipped (not failed) where no device is visible, so a
     # plain `pytest tests/` on a CPU-only machine stays green.
     try:
