@@ -21,7 +21,9 @@
  *   lse_i = log(sum over seen j of exp s(i, j));  p(i, j) = exp(s(i, j) - lse_i);  out_i = sum p v_j
  * A row that sees no key gives zeros and an lse of -infinity.  Keys and values that a row does
  * not see have no influence on it, whatever they hold (infinities and NaN too; rows that meet such
- * values are summed again one key at a time, which takes tens of times as long).  Positions:
+ * values, or share a tile's keys with rows that do, are summed again one key at a time: a prompt
+ * whose rows all do takes 60 to 120 times as long, and a value that is hidden from a row costs it
+ * as much as one that it sees).  Positions:
  * shared key j has j, own key j has prefix_len + j unless key_pos is given, row i prefix_len + o
  * unless q_pos is given; distances count in 32 bits.
  *

@@ -63,7 +63,7 @@ __device__ __forceinline__ bool head_item(int id, int heads, int items, int &hea
 // products; keys and values of the next stage are fetched straight into LDS meanwhile.  A score costs about thirteen vector instructions
 // (two of them its exponential's and sum's, five a cap's) and a 16th of a matrix instruction for each 16 features: with 128 features the
 // vector unit is busy for 0.55 of the time and the matrix unit for 0.3, and the two overlap less than half.  4 x 8192 causal rows of 40 heads of 128
-// bf16 features: 3.8 ms capped (0.73 PFLOP/s), 3.2 ms not.  Tiles of 32 rows whose waves share the keys, for calls of few tiles:
+// bf16 features: 3.7 ms capped (0.75 PFLOP/s), 3.2 ms not.  Tiles of 32 rows whose waves share the keys, for calls of few tiles:
 // 920 f32 rows took 58 us, these 42, since each tile fetches the keys again.
 template <typename T, int NT, bool WIDE>
 __global__ void __launch_bounds__(64 * kSpanWaves, span_steps_waves(NT)) k_span_prompt(const SpanCall p) {
@@ -290,12 +290,13 @@ template <typename T> __global__ void __launch_bounds__(256) k_span_join(const S
     if (j + e < p.c.most) out[j + e] = sum[e];
 }
 
-// attn_received.  A workgroup: a block of own keys of a request and KV head, 64 KB of them, or one from the front and one from the back, so
+// attn_received.  A workgroup: a block of KEYS own keys of a request and KV head, or one from the front and one from the back, so
 // that all workgroups have about the same number of rows to meet.  Half of its NW waves hold one half of the keys in registers, half the
 // other; a head's rows pass by through LDS, ROWS at a time, from the last to the first, so that the workgroups of an XCD meet the same rows
 // at about the same time.  What a key gets is summed in its lane over the rows, then over lanes and waves, in a fixed order.
 // Rows come from L2 for every block of keys: 64 keys of 128 bf16 features to a block made that the bound (4.5 TB/s), and 6007 capped rows of
-// 40 heads took 1.7 ms; with 128 keys it is the vector unit, as in attn_prompt at half the products a score, and 0.45 ms (0.41 PFLOP/s).
+// 40 heads took 1.7 ms; with 128 keys they take 0.42 (0.44 PFLOP/s), the vector unit busy for 0.51 of the time, the matrix unit for 0.18, and the waves
+// waiting for a third of theirs: eight waves a CU, and a barrier for every 128 rows.
 // Where few rows count (8 requests, their last 32 rows, 12 K keys) there is a stage to a workgroup, 26 us for two rounds of workgroups
 // that each wait for their keys.
 template <typename T, int NT, bool WIDE, int ROWS, int KB, int NW> struct Received {

@@ -522,6 +522,8 @@ template <typename T, int NT, int RW, int KW, int SKW, int NBUF, bool WIDE> stru
       t.l += sum;
     }
     if constexpr (ES == 2) {
+      // Probabilities are rounded to the matrix instruction's bf16, their sum is not: results of 128 bf16 features are 2.3e-3 from 64 bits
+      // instead of 1.7e-3, which rounding them alone takes.  In two parts of eight bits they would cost these products twice.
       auto add = [&](auto at) {  // 16 keys: their probabilities rounded, their values added, the next ones' operands fetched behind the products
         constexpr int AT = decltype(at)::value;
         bf16x8_t pf;

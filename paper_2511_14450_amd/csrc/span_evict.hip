@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(const EvictCall
 }
 
 // The same for up to 256 keys, and their move, in one launch: a key stays if fewer than `keep` come before it, counted one by one.  Latency
-// bounds it, 8 us for caches of 96 keys.  A call takes 13 us for 96 keys, 17 for 256; in two launches 17 for either, and for 512 (25 in one).
+// bounds it, 9 us for caches of 96 keys.  A call takes 12 us for 96 keys, 17 for 256; in two launches 17 for either, and for 512 (25 in one).
 constexpr int kSmall = kEvictSmall;
 template <bool VEC, int ES> __device__ void move_rows(const EvictCall &p, int b, int kvh, int r0, int rows, const int *kept, int threads);
 

@@ -38,9 +38,10 @@ inline SpanTokenPlan span_token_plan(int64_t requests, int64_t kv_heads, int64_t
 }
 
 // attn_received: whether a workgroup has a block of keys from the front and one from the back.  Causality gives the first keys the most rows, and
-// pairs of blocks even that out, of 128 keys, which fetch the rows half as often: 8 prompts of 2048 rows of 32 heads 290 instead of 350 us, one
-// of 4500 of 40 heads 337 instead of 399.  Not where all blocks meet as many rows (the last 512: 150 instead of 119), nor where the pairs do
-// not fill the chip (one prompt of 3500 rows, 140 of them: 276 instead of 263; 2048, 80: 183, 165).
+// pairs of blocks even that out, of 128 keys, which fetch the rows half as often: 8 prompts of 2048 rows of 32 heads 300 instead of 370 us, one
+// of 4500 of 40 heads 327 instead of 397, of 6007 430 instead of 675.  Not where all blocks meet as many rows (the last 512 of 8 prompts of 512 to
+// 2048: 155 instead of 128), nor where the pairs do not fill the chip (one prompt of 3500 rows, 140 of them: 268 instead of 254; 2048, 80:
+// 178, 158).  All rows of prompts of unequal length lose by it, which the host does not know (those of 512 to 2048: 274 instead of 248).
 inline bool span_received_pairs(int64_t most, int64_t last, int64_t requests, int64_t kv_heads, int64_t group) {
   const int64_t counts = last ? std::min(last, most) : most, pairs = (most + 255) / 256 * requests * kv_heads;
   return 2 * counts > most && counts * group > 512 && pairs >= 160;
