@@ -66,7 +66,7 @@ class SharedBlocks:
         self.lens = [torch.zeros(n_requests, dtype=torch.int32, device="cuda") for _ in layers]
         self.caches = [attn.AttnCache(k, v, n, prefix_k=p[0], prefix_v=p[1], key_pos=pos)
                        for k, v, n, p, pos in zip(self.k, self.v, self.lens, self.prefix, self.pos)]
-        self.now = torch.zeros(n_requests, dtype=torch.int32, device="cuda")  # position of the next token
+        self.now = torch.full((n_requests,), self.prefix_len, dtype=torch.int32, device="cuda")  # position of the next token
         self.most = 0  # keys that the longest request holds
         self.requests = torch.arange(n_requests, device="cuda")
 
