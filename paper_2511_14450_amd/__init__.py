@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     hyp_measure_hbm_read_ceiling, hypsplit_dp, hypsched_rt, hypsched_simulate,
 )
 from .attn import (  # noqa: F401
-    AttnCache, AttnRule, attn_evict, attn_last_error, attn_prompt, attn_received, attn_token, attn_workspace_bytes,
+    AttnCache, AttnRule, attn_evict, attn_evict_workspace_bytes, attn_last_error, attn_prompt, attn_received, attn_token, attn_workspace_bytes,
 )
 
 

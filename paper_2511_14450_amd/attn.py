@@ -294,6 +294,11 @@ def attn_received(cache: AttnCache, rule: AttnRule, q: torch.Tensor, q_start: to
     return totals if totals_out is None else totals_out
 
 
+def attn_evict_workspace_bytes(cache: AttnCache, keep: int) -> int:
+    """Bytes of workspace of attn_evict."""
+    return int(_lib().attn_evict_workspace_bytes(cache._ref, _int32(keep, "keep")))
+
+
 def attn_evict(cache: AttnCache, totals: torch.Tensor, keep: int, sink: int = 0, recent: int = 0, now: Optional[torch.Tensor] = None,
                into: Optional[AttnCache] = None, totals_out: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:

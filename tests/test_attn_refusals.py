@@ -160,3 +160,11 @@ def test_calls_beyond_a_launch_are_refused():
     long = attn._Rows(q=4096, q_row_stride=256, q_head_stride=8, n_rows=1 << 21, n_q_heads=1 << 10, q_start=4096)
     heads = cache(n_requests=1, n_kv_heads=1 << 10, head_dim=8)
     assert lib.attn_prompt(C.byref(heads), C.byref(rule), C.byref(long), C.byref(OUT), 4096, 1 << 50, None) == ESHAPE
+
+
+def test_every_entry_point_has_its_name_in_the_package():
+    import paper_2511_14450_amd as hyp
+    assert all(hasattr(hyp, name) for name in attn.EXPORTS_ATTN)
+    c = attn.AttnCache(f32(3, 2, 16, 64), f32(3, 2, 16, 64), i32(3))
+    assert hyp.attn_evict_workspace_bytes(c, 5) == 3 * 2 * 2 * 5 * 4  # two numbers a slot that stays
+    assert hyp.attn_evict_workspace_bytes(c, 0) == 0                   # refused
