@@ -259,11 +259,10 @@ def prepare(case, seed):
     if case["op"] == "read":
         s["out_k"], s["out_v"] = (torch.zeros((n, nkv, max(held), d), dtype=dt, device="cuda") for _ in range(2))
     if case["op"] == "select":  # selecting looks at bounds alone: the least that a cache has for keys
+        pages, size = (n * x["table"].shape[1], case["page"]) if case["page"] else (n, x["room"])
         for name, fmt in (("k", case["k_format"]), ("v", case["v_format"])):
-            s[name] = torch.zeros((1, 1, 1, _width(fmt, d)), dtype=torch.uint8, device="cuda")
-            s[name + "s"] = torch.zeros((1, 1, -(-d // 32), 1), dtype=torch.uint8, device="cuda")
-            pages, size = (n * x["table"].shape[1], case["page"]) if case["page"] else (n, x["room"])
-            s[name], s[name + "s"] = s[name].expand(pages, nkv, size, -1), s[name + "s"].expand(pages, nkv, -1, size)
+            s[name] = torch.zeros((1, 1, 1, _width(fmt, d)), dtype=torch.uint8, device="cuda").expand(pages, nkv, size, -1)
+            s[name + "s"] = torch.zeros((1, 1, 1, size), dtype=torch.uint8, device="cuda").expand(pages, nkv, -(-d // 32), -1)
     if case["slopes"]:
         s["slopes"] = torch.tensor(_slopes(case), dtype=torch.float32, device="cuda")
     if own:  # the descriptions of the tensors above that a program keeps with them: no values, nothing computed
