@@ -1,34 +1,12 @@
 // C entry points of hyp_attn.h: checks of the arguments and the cut of a call into launches.
-#include <cmath>
-#include <limits>
-#include <new>
-#include <string>
-
+#include "attn_rule.h"
 #include "span_kernels.h"
 #include "span_rules.h"
 
 namespace hyp {
 namespace {
 
-thread_local std::string t_error;
-constexpr float kLog2e = 1.4426950408889634f;
-
-struct Refused {
-  hyp_status_t status;
-  const char *text;
-};
-inline void need(bool ok, hyp_status_t status, const char *text) {
-  if (!ok) throw Refused{status, text};
-}
-
 int es_of(const hyp_attn_cache_t &c) { return c.dtype == HYP_BF16 ? 2 : 4; }
-
-// A launch has fewer than 2^32 lanes; one that is refused would leave the launches after it without what it writes.
-void check_launch(int64_t workgroups, int threads) { need(workgroups < (1ll << 32) / threads, HYP_ESHAPE, "too much work for a launch"); }
-
-bool apart(int64_t stride, int64_t n) { return n <= 1 || stride != 0; }
-
-bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
 
 int shift_of(const hyp_attn_cache_t &c) {
   int s = 0;
@@ -54,13 +32,6 @@ void check_cache(const hyp_attn_cache_t *c) {
     need(c->n_pages >= 1 && c->pages_per_request >= 1, HYP_ESHAPE, "cache: pages_per_request and n_pages must be positive");
     need((int64_t)c->pages_per_request * c->page_keys >= c->most, HYP_ESHAPE, "cache: pages_per_request * page_keys is below most");
   }
-}
-
-void check_rule(const hyp_attn_rule_t *r) {
-  need(r, HYP_EINVAL, "rule is null");
-  need(std::isfinite(r->scale) && r->scale > 0.f, HYP_EINVAL, "rule: scale must be finite and positive");
-  need(std::isfinite(r->cap) && r->cap >= 0.f, HYP_EINVAL, "rule: cap must be finite and not negative");
-  need(r->cap > 0.f || std::isfinite(r->scale * kLog2e), HYP_EINVAL, "rule: scale must be below 2.3e38 where scores are not capped");
 }
 
 void check_rows(const hyp_attn_cache_t &c, const hyp_attn_rows_t *r, bool token) {
@@ -115,23 +86,6 @@ SpanCall begin(const hyp_attn_cache_t &c, const hyp_attn_rows_t &r) {
   p.q_doc = r.q_doc;
   if (!r.q_doc) p.c.key_doc = nullptr;  // rows without ids see every id
   return p;
-}
-
-void add_rule(SpanCall &p, const hyp_attn_rule_t &rule) {
-  p.scale2 = rule.scale * kLog2e;
-  if (rule.cap > 0.f) {
-    p.to_cap = std::min(rule.scale / rule.cap, std::numeric_limits<float>::max());  // a score of 0 stays one under the smallest caps
-    p.cap2 = rule.cap * kLog2e;
-    // tanh(x) / x in powers of x^2 up to |x| = 0.4, of least relative error (9.8e-8); up to 0.5 the same error takes a power more, and an
-    // instruction more of the thirteen that a score costs
-    constexpr double tanh_c[4] = {0.9999999019048974, -0.3333136247072489, 0.13270976813015187, -0.04755360235665809};
-    const double k = (double)rule.scale / rule.cap;
-    double f = (double)rule.scale * kLog2e;
-    for (int i = 0; i < 4; ++i, f *= k * k) p.cap_c[i] = (float)(f * tanh_c[i]);
-    p.cap_most = (float)(0.4 / k);
-    if (!std::isfinite(p.cap_c[3])) p.cap_most = -1.f;  // a cap so far below the scale that tanh is 0 or 1
-  }
-  p.slopes = rule.slopes;
 }
 
 void add_out(SpanCall &p, const hyp_attn_out_t *o) {
@@ -207,34 +161,10 @@ void add_workspace(SpanCall &p, const Plan &w, void *workspace, size_t bytes) {
   p.part_ml = p.part_o + w.part_o;
 }
 
-void run(hipError_t e) {
-  if (e != hipSuccess) {
-    t_error = std::string("HIP: ") + hipGetErrorString(e);
-    throw Refused{HYP_EDEVICE, nullptr};
-  }
-}
-
 void join(SpanCall &p, hipStream_t s) {
   if (!p.part_o) return;
   p.join_items = (int)((p.n_rows * p.nq + 3) / 4);
   run(p.c.dtype == HYP_BF16 ? span_join<bf16_t>(p, s) : span_join<float>(p, s));
-}
-
-// No exception may cross the C ABI.
-template <typename F> hyp_status_t guarded(F &&body) {
-  try {
-    try {
-      body();
-      return HYP_OK;
-    } catch (const Refused &r) {
-      if (r.text) t_error = r.text;
-      return r.status;
-    }
-  } catch (const std::bad_alloc &) {
-    return HYP_ENOMEM;
-  } catch (...) {
-    return HYP_EDEVICE;
-  }
 }
 
 }  // namespace

@@ -6,13 +6,14 @@
 // registers in the order in which O^T += V^T P^T wants them, if that product's keys are taken in the same order.
 #pragma once
 
+#include "attn_score.h"
 #include "mfma_common.h"
 #include "span_kernels.h"
 
 namespace hyp {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = (float)(1.4426950408889634 - (double)kLog2e), kLn2 = 0.6931471805599453f;
+constexpr float kLog2eLow = (float)(1.4426950408889634 - (double)kLog2e), kLn2 = 0.6931471805599453f;
 constexpr float kFollow = 8.0f;  // the running maximum moves when a score passes it by more than 2^8
 
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16v4_t;
@@ -29,7 +30,6 @@ __device__ __forceinline__ float half_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 // This file is compiled as if no number were NaN, so that a maximum is one instruction.  Where a NaN may stand it is looked at
 // as an integer, which the compiler is kept from seeing through.
 __device__ __forceinline__ unsigned bits_of(float x) {
@@ -60,21 +60,6 @@ __device__ __forceinline__ int wave_max(int v) {  // not the negated minimum: -2
   return v;
 }
 __device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
-
-// A raw score S as an exponent of two, cap log2(e) tanh(S scale / cap).  With x = S scale / cap up to 0.4 in absolute value that is
-// S r(S^2), r a polynomial fitted to an even relative error (1e-7, and 1e-7 of its evaluation), whose coefficients the host scales;
-// beyond, 1 - 2 / (e^2x + 1), whose absolute error of one rounding is relative there.
-__device__ __forceinline__ float cap_factor(float s, const float (&c)[4]) {
-  const float y = s * s;
-  float q = fmaf(y, c[3], c[2]);
-  q = fmaf(y, q, c[1]);
-  return fmaf(y, q, c[0]);
-}
-__device__ __forceinline__ float cap_any(float s, const float (&c)[4], float most, float to_cap, float cap2) {
-  const float e = exp2_(2.0f * kLog2e * fabsf(s * to_cap));  // infinity: tanh is 1
-  const float far = copysignf(cap2 - 2.0f * cap2 * __builtin_amdgcn_rcpf(e + 1.0f), s);
-  return fabsf(s) <= most ? s * cap_factor(s, c) : far;
-}
 
 __device__ __forceinline__ float load_val(const float *p) { return *p; }
 __device__ __forceinline__ float load_val(const bf16_t *p) { return bf16_to_f32(*p); }
