@@ -1,7 +1,7 @@
 """MI355X-native forward pass of one pipeline stage of decoder blocks.
 
 The work is done by the HIP library `libhyp_stage.so` (C ABI in
-include/hyp_stage.h, hyp_plan.h and hyp_attn.h); this package only marshals arguments.  Importing the
+include/hyp_stage.h, hyp_plan.h, hyp_attn.h and hyp_mx.h); this package only marshals arguments.  Importing the
 package does not load the library; the first call does, and fails loudly if it
 has not been built (python -m paper_2511_14450_amd.build).
 """
@@ -14,6 +14,9 @@ from .binding import (  # noqa: F401
 )
 from .attn import (  # noqa: F401
     AttnCache, AttnRule, attn_evict, attn_evict_workspace_bytes, attn_last_error, attn_prompt, attn_received, attn_token, attn_workspace_bytes,
+)
+from .mx import (  # noqa: F401
+    MxCache, mx_last_error, mx_read, mx_select, mx_select_workspace_bytes, mx_token, mx_token_workspace_bytes, mx_write,
 )
 
 

@@ -1,0 +1,348 @@
+// Which blocks of a request's keys a row reads.
+#include "mx_format.h"
+#include "mx_rules.h"
+
+namespace hyp {
+namespace {
+
+constexpr int kThreads = 256, kHeads = 4;  // query heads whose scores are formed at a time
+constexpr int kSelectThreads = 1024, kItems = 4, kMostCandidates = 1024;
+
+typedef unsigned long long u64;
+
+// Order of scores as unsigned numbers: -0 as 0, a NaN above all numbers.  0 and the highest are no score's: blocks that are not there, and
+// those that are always taken.
+__device__ __forceinline__ u64 order_of(double x) {
+  const u64 u = (u64)__double_as_longlong(x);
+  if ((u << 1) > 0xffe0000000000000ull) return ~0ull - 1;
+  if ((u << 1) == 0) return 1ull << 63;
+  return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
+}
+
+template <int X> __device__ __forceinline__ double row_xor(double v) {  // of the 16 lanes of a row
+  const u64 u = (u64)__double_as_longlong(v);
+  constexpr int ctrl = X == 1 ? 0xb1 : X == 2 ? 0x4e : X == 4 ? 0x141 : 0x128;  // quad_perm, quad_perm, row_half_mirror, row_ror:8
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, 0xf, 0xf, true);
+  const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, 0xf, 0xf, true);
+  return __longlong_as_double((long long)((u64)hi << 32 | lo));
+}
+
+template <typename T> __device__ __forceinline__ void load_q(const MxSelectCall &p, int b, int head, int f, double (&x)[8]) {
+  const int d = p.m.c.head_dim;
+  const T *q = (const T *)p.q.q + b * p.q.q_row_stride + head * p.q.q_head_stride;
+  if (p.wide_q && f < d) {
+    if constexpr (sizeof(T) == 2) {
+      const u16x8_t v = *(const u16x8_t *)(q + f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = (double)bf16_to_f32(v.v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = (double)q[f + i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = f + i < d ? (double)load_f32(q + f + i) : 0.0;
+}
+
+__device__ __forceinline__ void load_bound(const bf16_t *row, int f, int d, bool wide, float (&x)[8]) {
+  if (wide && f < d) {
+    const u16x8_t v = *(const u16x8_t *)(row + f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(v.v[i]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = f + i < d ? bf16_to_f32(row[f + i]) : 0.f;
+}
+
+__device__ __forceinline__ int64_t bound_at(const MxSelectCall &p, int b, int kvh, int i) {
+  const hyp_mx_cache_t &c = p.m.c;
+  if (!c.page_table) return (int64_t)b * c.bound_page_stride + kvh * c.bound_head_stride + i * c.bound_block_stride;
+  const int s = p.m.shift - p.m.block_shift;  // log2(blocks of a page)
+  const int page = mx_clamped(c.page_table[(int64_t)b * c.pages_per_request + (i >> s)], 0, c.n_pages - 1);
+  return (int64_t)page * c.bound_page_stride + kvh * c.bound_head_stride + (i & ((1 << s) - 1)) * c.bound_block_stride;
+}
+
+// Order of the scores of blocks i0, i0 + step, ... below i1 of one request and KV head: 16 lanes a block, LPL = 8 or 16 features a lane.
+// What is formed of 8-bit products in 64 bits is exact for all but wide spreads of sizes, so that the choice does not hang on the order of the sums.
+template <typename T, int PIECES, typename Put> __device__ __forceinline__ void score_blocks(const MxSelectCall &p, int b, int kvh, int i0, int i1, int step, Put &&put) {
+  const hyp_mx_cache_t &c = p.m.c;
+  const int lane = threadIdx.x & 15, d = c.head_dim, group = p.q.n_q_heads / c.n_kv_heads;
+  const bf16_t *lo = (const bf16_t *)c.lo, *hi = (const bf16_t *)c.hi;
+  for (int g0 = 0; g0 < group; g0 += kHeads) {
+    double q[kHeads][PIECES][8];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+#pragma unroll
+      for (int x = 0; x < PIECES; ++x) load_q<T>(p, b, kvh * group + min(g0 + h, group - 1), x * 128 + lane * 8, q[h][x]);
+    }
+    for (int i = i0; i < i1; i += step) {
+      const int64_t at = bound_at(p, b, kvh, i);
+      double sum[kHeads];
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) sum[h] = 0.0;
+#pragma unroll
+      for (int x = 0; x < PIECES; ++x) {
+        float l[8], u[8];
+        load_bound(lo + at, x * 128 + lane * 8, d, p.wide_bound, l);
+        load_bound(hi + at, x * 128 + lane * 8, d, p.wide_bound, u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const double a = (double)l[k], z = (double)u[k];
+#pragma unroll
+          for (int h = 0; h < kHeads; ++h) sum[h] = fma(q[h][x][k], q[h][x][k] >= 0.0 ? z : a, sum[h]);
+        }
+      }
+      u64 best = 0;
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        double v = sum[h];
+        v += row_xor<1>(v);
+        v += row_xor<2>(v);
+        v += row_xor<4>(v);
+        v += row_xor<8>(v);
+        best = max(best, order_of(v));
+      }
+      if (lane == 0) put(i, best, g0 > 0);
+    }
+  }
+}
+
+template <typename T, int PIECES> __global__ void __launch_bounds__(kThreads) k_mx_scores(const MxSelectCall p, int tiles, int tile_blocks) {
+  const int tile = blockIdx.x % tiles, pair = blockIdx.x / tiles, b = pair / p.m.c.n_kv_heads, kvh = pair % p.m.c.n_kv_heads;
+  const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
+  if (count <= p.keep) return;
+  const int i0 = tile * tile_blocks, i1 = min(count, i0 + tile_blocks);
+  u64 *order = p.order + (int64_t)pair * p.most_blocks;
+  score_blocks<T, PIECES>(p, b, kvh, i0 + (threadIdx.x >> 4), i1, kThreads / 16, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
+}
+
+// sum of v over the threads before this one, and over all; scratch: one int a wave
+template <int WAVES> __device__ __forceinline__ int before_me(int v, int *scratch, int &all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = v;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int x = __shfl_up(upto, s);
+    if (lane >= s) upto += x;
+  }
+  if (lane == 63) scratch[wave] = upto;
+  __syncthreads();
+  int before = upto - v;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    before += w < wave ? scratch[w] : 0;
+    all += scratch[w];
+  }
+  __syncthreads();
+  return before;
+}
+
+// One request and KV head with more blocks than are kept.  Scores are sorted into 2048 bins between the least and the largest; the bin in which
+// the last one falls that is taken is cut into 2048 again until it holds few, which are then ranked one by one.
+__global__ void __launch_bounds__(kSelectThreads) k_mx_choose(const MxSelectCall p) {
+  constexpr int WAVES = kSelectThreads / 64;
+  __shared__ int hist[2048], scratch[WAVES], found[3];
+  __shared__ u64 ends[2], cand[kMostCandidates];
+  __shared__ int cand_at[kMostCandidates];
+  const int pair = blockIdx.x, b = pair / p.m.c.n_kv_heads, tid = threadIdx.x, lane = tid & 63, K = p.keep;
+  const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
+  int *out = p.blocks + (int64_t)pair * K;
+  if (count <= K) {
+    for (int r = tid; r < K; r += kSelectThreads) out[r] = r < count ? r : -1;
+    return;
+  }
+  const u64 *order = p.order + (int64_t)pair * p.most_blocks;
+  const int newest = count - p.recent;
+  // a thread has runs of kItems blocks, so that counts in the order of threads are counts in the order of blocks
+  constexpr int STEP = kSelectThreads * kItems;
+  const bool once = count <= STEP;
+  u64 u[kItems];
+  auto read = [&](int base) {
+#pragma unroll
+    for (int x = 0; x < kItems; ++x) {
+      const int i = base + tid * kItems + x;
+      u[x] = i >= count ? 0 : (i < p.sink || i >= newest) ? ~0ull : order[i];
+    }
+  };
+  auto each = [&](auto &&f) {  // f(block, its order), for those with a score of their own
+    for (int base = 0; base < count; base += STEP) {
+      if (!once) read(base);
+#pragma unroll
+      for (int x = 0; x < kItems; ++x)
+        if (u[x] != 0 && u[x] != ~0ull) f(base + tid * kItems + x, u[x]);
+    }
+  };
+  if (once) read(0);
+  const int always = p.sink + p.recent;
+  int need = K - always;  // of the others; no block is both, for count > K >= always
+  u64 from = ~0ull, to = 0;
+  if (tid == 0) {
+    ends[0] = ~0ull;
+    ends[1] = 0;
+  }
+  __syncthreads();
+  each([&](int, u64 v) {
+    from = min(from, v);
+    to = max(to, v);
+  });
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    from = min(from, (u64)__shfl_xor((long long)from, s));
+    to = max(to, (u64)__shfl_xor((long long)to, s));
+  }
+  if (lane == 0) {
+    atomicMin(&ends[0], from);
+    atomicMax(&ends[1], to);
+  }
+  __syncthreads();
+  from = ends[0];
+  to = ends[1];
+  // taken: all above `to`, and `need` of [from, to]
+  int inside = count - always;
+  while (need > 0 && need < inside && inside > kMostCandidates && from < to) {
+    const int shift = max(0, 64 - __clzll((long long)(to - from)) - 11);
+    for (int x = tid; x < 2048; x += kSelectThreads) hist[x] = 0;
+    __syncthreads();
+    each([&](int, u64 v) {
+      if (v >= from && v <= to) atomicAdd(&hist[(int)((v - from) >> shift)], 1);
+    });
+    __syncthreads();
+    const int hi = 2047 - 2 * tid, own0 = hist[hi], own1 = hist[hi - 1];
+    int all;
+    const int above = before_me<WAVES>(own0 + own1, scratch, all);
+    if (above < need && need <= above + own0) {
+      found[0] = hi;
+      found[1] = above;
+      found[2] = own0;
+    } else if (above + own0 < need && need <= above + own0 + own1) {
+      found[0] = hi - 1;
+      found[1] = above + own0;
+      found[2] = own1;
+    }
+    __syncthreads();
+    need -= found[1];
+    inside = found[2];
+    const u64 base = from + ((u64)found[0] << shift);
+    if (to - base >= 1ull << shift) to = base + ((1ull << shift) - 1);
+    from = base;
+    __syncthreads();
+  }
+  // of [from, to] `need` are taken: none, all, the first ones where all are equal, or the best by rank
+  u64 last = from;       // least order that is taken
+  int equal = 0x7fffffff;  // how many of that order are, from the first block on
+  if (need <= 0) {
+    last = to + 1;
+  } else if (need < inside) {
+    if (from == to) {
+      equal = need;
+    } else {
+      if (tid == 0) found[0] = 0;
+      __syncthreads();
+      each([&](int i, u64 v) {
+        if (v >= from && v <= to) {
+          const int x = atomicAdd(&found[0], 1);
+          cand[x] = v;
+          cand_at[x] = i;
+        }
+      });
+      __syncthreads();
+      if (tid < inside) {
+        const u64 mine = cand[tid];
+        const int at = cand_at[tid];
+        int before = 0, same = 0;
+        for (int x = 0; x < inside; ++x) {
+          const u64 v = cand[x];
+          before += v > mine || (v == mine && cand_at[x] < at);
+          same += v == mine && cand_at[x] < at;
+        }
+        if (before == need - 1) {  // the last one that is taken
+          ends[0] = mine;
+          found[1] = same + 1;
+        }
+      }
+      __syncthreads();
+      last = ends[0];
+      equal = found[1];
+    }
+  }
+  int done = 0, equals = 0;
+  for (int base = 0; base < count; base += STEP) {
+    if (!once) read(base);
+    int mine = 0, all;
+#pragma unroll
+    for (int x = 0; x < kItems; ++x) mine += u[x] == last;
+    int nth = equals + before_me<WAVES>(mine, scratch, all);
+    equals += all;
+    int taken = 0;
+    unsigned which = 0;
+#pragma unroll
+    for (int x = 0; x < kItems; ++x) {
+      const bool is = u[x] == last;
+      const bool t = u[x] == ~0ull || (u[x] != 0 && (u[x] > last || (is && nth < equal)));
+      nth += is;
+      which |= (unsigned)t << x;
+      taken += t;
+    }
+    int at = done + before_me<WAVES>(taken, scratch, all);
+    done += all;
+#pragma unroll
+    for (int x = 0; x < kItems; ++x)
+      if ((which >> x) & 1) out[at++] = base + tid * kItems + x;
+  }
+}
+
+// The same for requests of up to 256 blocks, scores and choice in one launch: a block is taken if fewer than `keep` come before it.
+template <typename T, int PIECES> __global__ void __launch_bounds__(kThreads) k_mx_select_small(const MxSelectCall p) {
+  __shared__ u64 order[kMxSmallBlocks];
+  __shared__ int scratch[kThreads / 64];
+  const int pair = blockIdx.x, b = pair / p.m.c.n_kv_heads, kvh = pair % p.m.c.n_kv_heads, tid = threadIdx.x, K = p.keep;
+  const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
+  int *out = p.blocks + (int64_t)pair * K;
+  if (count <= K) {
+    for (int r = tid; r < K; r += kThreads) out[r] = r < count ? r : -1;
+    return;
+  }
+  score_blocks<T, PIECES>(p, b, kvh, tid >> 4, count, kThreads / 16, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
+  __syncthreads();
+  if (tid >= count) order[tid] = 0;
+  else if (tid < p.sink || tid >= count - p.recent) order[tid] = ~0ull;
+  __syncthreads();
+  const u64 mine = order[tid];
+  int before = 0;
+  for (int i = 0; i < count; ++i) {
+    const u64 v = order[i];
+    before += v > mine || (v == mine && i < tid);
+  }
+  const int taken = tid < count && before < K;
+  int all;
+  const int at = before_me<kThreads / 64>(taken, scratch, all);
+  if (taken) out[at] = tid;
+}
+
+template <typename T, int PIECES> hipError_t select(const MxSelectCall &p, hipStream_t s) {
+  const unsigned pairs = (unsigned)p.m.c.n_requests * p.m.c.n_kv_heads;
+  if (mx_select_once(p.most_blocks, p.keep)) {
+    k_mx_select_small<T, PIECES><<<pairs, kThreads, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  const int tiles = (p.most_blocks + kMxScoreBlocks - 1) / kMxScoreBlocks;
+  k_mx_scores<T, PIECES><<<pairs * tiles, kThreads, 0, s>>>(p, tiles, kMxScoreBlocks);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;  // the choice goes by the scores
+  k_mx_choose<<<pairs, kSelectThreads, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <typename T> hipError_t mx_select(const MxSelectCall &p, hipStream_t s) {
+  return p.m.c.head_dim <= 128 ? select<T, 1>(p, s) : select<T, 2>(p, s);
+}
+
+template hipError_t mx_select<float>(const MxSelectCall &, hipStream_t);
+template hipError_t mx_select<bf16_t>(const MxSelectCall &, hipStream_t);
+
+}  // namespace hyp
