@@ -56,7 +56,7 @@ typedef enum { HYP_E4M3 = 0, HYP_E2M1 = 1 } hyp_mx_format_t;
  * Pages: page = page_table[b * pages_per_request + j / page_keys] instead of b and j % page_keys
  *   instead of j; page_keys is a power of two, 16 at least; pages_per_request * page_keys >= most.
  * k, v, and their strides are multiples of 16; k_scale, v_scale and their strides multiples of 4; key
- * strides lie in 0..2^24 - 1.
+ * strides lie in 0..2^24 - 1, group strides in 0..2^28 - 1.
  * Bounds: lo and hi (bf16) hold the least and the largest number of each feature over the keys of a
  *   block, blocks being block_keys keys from key 0 on: those of block i at
  *   lo + page * bound_page_stride + c * bound_head_stride + (i % blocks of a page) * bound_block_stride

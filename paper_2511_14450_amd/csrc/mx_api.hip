@@ -40,6 +40,8 @@ MxCache check_cache(const hyp_mx_cache_t *c) {
   need(aligned(c->k_scale, 4) && aligned(c->v_scale, 4) && c->k_scale_page_stride % 4 == 0 && c->k_scale_head_stride % 4 == 0 &&
            c->k_scale_group_stride % 4 == 0 && c->v_scale_page_stride % 4 == 0 && c->v_scale_head_stride % 4 == 0 && c->v_scale_group_stride % 4 == 0,
        HYP_EINVAL, "cache: k_scale, v_scale or a stride of theirs is no multiple of 4 bytes");
+  need(c->k_scale_group_stride >= 0 && c->k_scale_group_stride < (1 << 28) && c->v_scale_group_stride >= 0 && c->v_scale_group_stride < (1 << 28), HYP_ESHAPE,
+       "cache: group strides of scales must be 0..2^28 - 1");
   need((c->lo == nullptr) == (c->hi == nullptr), HYP_EINVAL, "cache: lo and hi go together");
   need(aligned(c->lo, 2) && aligned(c->hi, 2), HYP_EINVAL, "cache: lo or hi is not aligned to its elements");
   need(!c->lo || c->block_keys, HYP_EINVAL, "cache: bounds without block_keys");
@@ -96,11 +98,12 @@ Plan plan_token(const MxCache &m, const hyp_mx_q_t &q, int32_t listed) {
   p.group = q.n_q_heads / c.n_kv_heads;
   p.head_tiles = (p.group + 15) / 16;
   p.items = (int64_t)c.n_requests * c.n_kv_heads * p.head_tiles;
-  p.cut = mx_token_plan(p.items, listed ? (int64_t)listed << (m.block_shift - 4) : ((int64_t)c.most + 15) / 16);
+  p.cut = mx_token_plan(p.items, listed ? (int64_t)listed << m.block_shift : c.most, c.page_keys, listed ? c.block_keys : 0,
+                        m.groups * ((c.k_format == HYP_E4M3 ? 32 : 16) + (c.v_format == HYP_E4M3 ? 32 : 16) + 2), q.dtype == HYP_F32);
   check_launch(p.items * p.cut.parts, 256);
   if (p.cut.parts > 1) {
     const int64_t rows = (int64_t)c.n_requests * q.n_q_heads;
-    check_launch((rows + 3) / 4, 256);
+    check_launch(rows, 256);
     p.part_o = (p.cut.parts * rows * c.head_dim + 3) / 4 * 4;
     p.part_ml = 2 * p.cut.parts * rows;
   }
@@ -268,7 +271,8 @@ hyp_status_t mx_token(const hyp_mx_cache_t *cache, const hyp_attn_rule_t *rule, 
     p.lse = out->lse;
     p.G = w.group;
     p.head_tiles = w.head_tiles;
-    p.runs = w.cut.runs;
+    p.unit = w.cut.unit;
+    p.units = w.cut.units;
     p.parts = w.cut.parts;
     if (w.bytes()) {
       p.part_o = (float *)workspace;

@@ -17,15 +17,33 @@ inline int64_t mx_write_tiles(int64_t rows, int64_t requests, int64_t block, boo
 constexpr int kMxSmallBlocks = 256, kMxScoreBlocks = 64;  // else blocks of a workgroup that forms scores
 inline bool mx_select_once(int blocks, int keep) { return blocks <= kMxSmallBlocks || blocks <= keep; }
 
-// mx_token: runs of 16 keys (of one page, or of one listed block) of a part, and parts of a request.
-constexpr int kMxMostRuns = 512;     // of a part: their places lie in LDS
-struct MxTokenPlan { int runs, parts; };
-inline MxTokenPlan mx_token_plan(int64_t items, int64_t runs) {
-  // 512 workgroups, but no part of less than 256 keys, which is 8 runs for two waves of four
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>((512 + items - 1) / items, (runs + 15) / 16));
-  int64_t each = (runs + parts - 1) / parts;
-  each = std::min<int64_t>((each + 7) / 8 * 8, kMxMostRuns);
-  return {(int)each, (int)((runs + each - 1) / each)};
+// mx_token: units of 32 keys, or of 16 where pages or listed blocks are so short, of a part, and parts of a request.
+constexpr int kMxMostUnits = 256;    // of a part: their places lie in LDS
+struct MxTokenPlan { int unit, units, parts; };  // unit: log2 of its keys
+// Of one part a request, as many parts as give one workgroup a CU, and as many as give two, the one that a call is estimated to take the least time
+// with, by what was measured: a workgroup alone on a CU goes through 125 keys a us (f32 rows: 65) and two through 170 (85) together, as far
+// as a CU's 24 KB a us last; joining parts takes 6 us.  Eight heads of 8 x 32768 keys of 128 features: e4m3 in 256 / 512 workgroups 92 / 96 us,
+// e2m1 66 / 54, of 64 features 74 / 56; eight of 8 x 512 keys in one part 13, in two 18; ten heads of 24 x 2048 keys (e4m3, e2m1) in one part
+// 23, in two 29.  No part has fewer than 256 keys, and more workgroups than have room at once (2 a CU) wait for others to end.
+inline MxTokenPlan mx_token_plan(int64_t items, int64_t keys, int64_t page_keys, int64_t block_keys, int64_t key_bytes, bool f32) {
+  MxTokenPlan t = {};
+  t.unit = page_keys % 32 == 16 || block_keys == 16 ? 4 : 5;  // page_keys: also the room of a slab; block_keys: 0 where none are listed
+  const int64_t units = (keys + (1 << t.unit) - 1) >> t.unit;
+  const int64_t cu = 24000 / key_bytes, alone = std::min<int64_t>(cu, f32 ? 65 : 125), two = std::min<int64_t>(cu, f32 ? 85 : 170);  // keys a us
+  int64_t parts = 1, least = 0;
+  for (int64_t places : {int64_t(0), int64_t(256), int64_t(512)}) {
+    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(places / items, keys / 256));
+    const int64_t time = (n * items <= 256 ? keys * 1000 / (n * alone) : keys * 2000 / (n * two)) + (n > 1 ? 6000 : 0);
+    if (places == 0 || time < least) {
+      parts = n;
+      least = time;
+    }
+  }
+  int64_t each = (units + parts - 1) / parts;
+  each = std::min<int64_t>((each + 7) / 8 * 8, kMxMostUnits);
+  t.units = (int)each;
+  t.parts = (int)((units + each - 1) / each);
+  return t;
 }
 
 }  // namespace hyp

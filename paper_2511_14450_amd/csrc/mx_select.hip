@@ -6,7 +6,7 @@ namespace hyp {
 namespace {
 
 constexpr int kThreads = 256, kHeads = 4;  // query heads whose scores are formed at a time
-constexpr int kSelectThreads = 1024, kItems = 4, kMostCandidates = 1024;
+constexpr int kSelectThreads = 1024, kItems = 4, kMostCandidates = kSelectThreads / 8;
 
 typedef unsigned long long u64;
 
@@ -45,16 +45,15 @@ template <typename T> __device__ __forceinline__ void load_q(const MxSelectCall 
   for (int i = 0; i < 8; ++i) x[i] = f + i < d ? (double)load_f32(q + f + i) : 0.0;
 }
 
-__device__ __forceinline__ void load_bound(const bf16_t *row, int f, int d, bool wide, float (&x)[8]) {
-  if (wide && f < d) {
-    const u16x8_t v = *(const u16x8_t *)(row + f);
+// Features f .. f + 7 of a block's bound, two a word, as they lie in memory
+__device__ __forceinline__ uint4 load_bound(const bf16_t *row, int f, int d, bool wide) {
+  if (wide && f < d) return *(const uint4 *)(row + f);
+  unsigned w[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(v.v[i]);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = f + i < d ? bf16_to_f32(row[f + i]) : 0.f;
+  for (int i = 0; i < 4; ++i) w[i] = (f + 2 * i < d ? row[f + 2 * i] : 0u) | (f + 2 * i + 1 < d ? row[f + 2 * i + 1] : 0u) << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ unsigned word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 __device__ __forceinline__ int64_t bound_at(const MxSelectCall &p, int b, int kvh, int i) {
   const hyp_mx_cache_t &c = p.m.c;
@@ -64,47 +63,70 @@ __device__ __forceinline__ int64_t bound_at(const MxSelectCall &p, int b, int kv
   return (int64_t)page * c.bound_page_stride + kvh * c.bound_head_stride + (i & ((1 << s) - 1)) * c.bound_block_stride;
 }
 
-// Order of the scores of blocks i0, i0 + step, ... below i1 of one request and KV head: 16 lanes a block, LPL = 8 or 16 features a lane.
-// What is formed of 8-bit products in 64 bits is exact for all but wide spreads of sizes, so that the choice does not hang on the order of the sums.
+// Order of the scores of blocks i0, i0 + step, ... below i1 of one request and KV head: 16 lanes a block, eight features a lane (PIECES times),
+// kBatch blocks at a time, whose bounds are all requested before the first is used.  What is formed of 8-bit products in 64 bits is exact for all
+// but wide spreads of sizes, so that the choice does not hang on the order of the sums.
 template <typename T, int PIECES, typename Put> __device__ __forceinline__ void score_blocks(const MxSelectCall &p, int b, int kvh, int i0, int i1, int step, Put &&put) {
+  constexpr int kBatch = 4 / PIECES;
   const hyp_mx_cache_t &c = p.m.c;
   const int lane = threadIdx.x & 15, d = c.head_dim, group = p.q.n_q_heads / c.n_kv_heads;
   const bf16_t *lo = (const bf16_t *)c.lo, *hi = (const bf16_t *)c.hi;
   for (int g0 = 0; g0 < group; g0 += kHeads) {
     double q[kHeads][PIECES][8];
+    unsigned up[kHeads][PIECES][4];  // where a feature's largest number counts, else its least: two a word, as the bounds
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
 #pragma unroll
-      for (int x = 0; x < PIECES; ++x) load_q<T>(p, b, kvh * group + min(g0 + h, group - 1), x * 128 + lane * 8, q[h][x]);
-    }
-    for (int i = i0; i < i1; i += step) {
-      const int64_t at = bound_at(p, b, kvh, i);
-      double sum[kHeads];
+      for (int x = 0; x < PIECES; ++x) {
+        load_q<T>(p, b, kvh * group + min(g0 + h, group - 1), x * 128 + lane * 8, q[h][x]);
 #pragma unroll
-      for (int h = 0; h < kHeads; ++h) sum[h] = 0.0;
+        for (int k = 0; k < 4; ++k)
+          up[h][x][k] = (q[h][x][2 * k] >= 0.0 ? 0xffffu : 0u) | (q[h][x][2 * k + 1] >= 0.0 ? 0xffff0000u : 0u);
+      }
+    }
+    for (int first = i0; first < i1; first += step * kBatch) {
+      int64_t at[kBatch];
+#pragma unroll
+      for (int n = 0; n < kBatch; ++n) at[n] = bound_at(p, b, kvh, min(first + n * step, i1 - 1));
+      double sum[kBatch][kHeads];
+#pragma unroll
+      for (int n = 0; n < kBatch; ++n)
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) sum[n][h] = 0.0;
 #pragma unroll
       for (int x = 0; x < PIECES; ++x) {
-        float l[8], u[8];
-        load_bound(lo + at, x * 128 + lane * 8, d, p.wide_bound, l);
-        load_bound(hi + at, x * 128 + lane * 8, d, p.wide_bound, u);
+        uint4 l[kBatch], u[kBatch];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const double a = (double)l[k], z = (double)u[k];
-#pragma unroll
-          for (int h = 0; h < kHeads; ++h) sum[h] = fma(q[h][x][k], q[h][x][k] >= 0.0 ? z : a, sum[h]);
+        for (int n = 0; n < kBatch; ++n) {
+          l[n] = load_bound(lo + at[n], x * 128 + lane * 8, d, p.wide_bound);
+          u[n] = load_bound(hi + at[n], x * 128 + lane * 8, d, p.wide_bound);
         }
-      }
-      u64 best = 0;
 #pragma unroll
-      for (int h = 0; h < kHeads; ++h) {
-        double v = sum[h];
-        v += row_xor<1>(v);
-        v += row_xor<2>(v);
-        v += row_xor<4>(v);
-        v += row_xor<8>(v);
-        best = max(best, order_of(v));
+        for (int n = 0; n < kBatch; ++n)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int h = 0; h < kHeads; ++h) {
+              const unsigned m = up[h][x][k], w = (word_of(u[n], k) & m) | (word_of(l[n], k) & ~m);
+              sum[n][h] = fma(q[h][x][2 * k], (double)__uint_as_float(w << 16), sum[n][h]);
+              sum[n][h] = fma(q[h][x][2 * k + 1], (double)__uint_as_float(w & 0xffff0000u), sum[n][h]);
+            }
       }
-      if (lane == 0) put(i, best, g0 > 0);
+#pragma unroll
+      for (int n = 0; n < kBatch; ++n) {
+        u64 best = 0;
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) {
+          double v = sum[n][h];
+          v += row_xor<1>(v);
+          v += row_xor<2>(v);
+          v += row_xor<4>(v);
+          v += row_xor<8>(v);
+          best = max(best, order_of(v));
+        }
+        const int i = first + n * step;
+        if (lane == 0 && i < i1) put(i, best, g0 > 0);
+      }
     }
   }
 }
@@ -249,19 +271,21 @@ __global__ void __launch_bounds__(kSelectThreads) k_mx_choose(const MxSelectCall
         }
       });
       __syncthreads();
-      if (tid < inside) {
-        const u64 mine = cand[tid];
-        const int at = cand_at[tid];
-        int before = 0, same = 0;
-        for (int x = 0; x < inside; ++x) {
-          const u64 v = cand[x];
-          before += v > mine || (v == mine && cand_at[x] < at);
-          same += v == mine && cand_at[x] < at;
-        }
-        if (before == need - 1) {  // the last one that is taken
-          ends[0] = mine;
-          found[1] = same + 1;
-        }
+      // eight threads a candidate, whose counts are joined by a butterfly
+      const int x0 = tid >> 3;
+      const u64 mine = x0 < inside ? cand[x0] : 0;
+      const int at = x0 < inside ? cand_at[x0] : 0;
+      int counts = 0;  // of those before it, and of those before it that are equal, in 16 bits each
+      for (int x = tid & 7; x < inside; x += 8) {
+        const u64 v = cand[x];
+        const bool same = v == mine && cand_at[x] < at;
+        counts += (v > mine || same ? 1 : 0) + (same ? 1 << 16 : 0);
+      }
+#pragma unroll
+      for (int x = 1; x < 8; x <<= 1) counts += __shfl_xor(counts, x);
+      if ((tid & 7) == 0 && x0 < inside && (counts & 0xffff) == need - 1) {  // the last one that is taken
+        ends[0] = mine;
+        found[1] = (counts >> 16) + 1;
       }
       __syncthreads();
       last = ends[0];

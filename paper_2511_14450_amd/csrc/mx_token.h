@@ -19,6 +19,7 @@ namespace hyp {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr bool kNtK = true, kNtV = true;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFollow = 8.0f;     // the running maximum moves when a score passes it by more than 2^8
 constexpr float kLowest = -3.402823466e38f;  // the maximum of no score: finite, so that a score of -infinity has the weight 0 beside it
@@ -40,19 +41,22 @@ template <int G, int F, bool KEY> struct Pieces {
 };
 constexpr int piece_bytes(int format, int feats) { return format == HYP_E4M3 ? feats : feats / 2; }
 
-template <int BYTES> __device__ __forceinline__ void load_bytes(const uint8_t *p, unsigned *w) {
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+template <int BYTES, bool NT> __device__ __forceinline__ void load_bytes(const uint8_t *p, unsigned *w) {
+  auto get = [](auto *at) { return NT ? __builtin_nontemporal_load(at) : *at; };
   if constexpr (BYTES == 16) {
-    const uint4 x = *(const uint4 *)p;
+    const u32x4_t x = get((const u32x4_t *)p);
     w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
   } else if constexpr (BYTES == 8) {
-    const uint2 x = *(const uint2 *)p;
+    const u32x2_t x = get((const u32x2_t *)p);
     w[0] = x.x; w[1] = x.y;
   } else if constexpr (BYTES == 4) {
-    w[0] = *(const unsigned *)p;
+    w[0] = get((const unsigned *)p);
   } else if constexpr (BYTES == 2) {
-    w[0] = *(const uint16_t *)p;
+    w[0] = get((const uint16_t *)p);
   } else {
-    w[0] = *p;
+    w[0] = get(p);
   }
 }
 constexpr int words(int bytes) { return (bytes + 3) / 4; }
@@ -102,13 +106,14 @@ template <typename T, int G, int KF, int VF> struct Token {
   struct Run {                 // of 16 keys, as a lane holds it
     unsigned k[KW], ks[KP.n];
     unsigned v[4][VW], vs[VP.n];
-    int valid;                 // keys that are there; 0: none
+    int valid;                 // keys that are there: none below 1, all from 16 on
     int first;                 // their first key
   };
 
   const MxTokenCall &p;
   const int lane, col, quarter;
-  int kvh;
+  // bytes from a run's first key to this lane's keys and values, and to their scales (key strides are below 2^24, group strides below 2^28)
+  unsigned k_at, v_at[4], ks_at[KP.n], vs_at[VP.n];
   bf16x8_t q[QP][G];
   f32x4_t o[2 * G];
   float m, l;
@@ -163,55 +168,54 @@ template <typename T, int G, int KF, int VF> struct Token {
     l = 0.f;
   }
 
-  // place: page (or request), place in it of the run's first key, keys that are there, first key.  Keys beyond the last one that is there are read
-  // as that one, of which nothing is used.
-  __device__ __forceinline__ void fetch(Run &r, int4 place) {
+  __device__ __forceinline__ void aim() {
     const hyp_mx_cache_t &c = p.m.c;
-    const int page = __builtin_amdgcn_readfirstlane(place.x), at = __builtin_amdgcn_readfirstlane(place.y);
-    r.valid = __builtin_amdgcn_readfirstlane(place.z);
-    r.first = __builtin_amdgcn_readfirstlane(place.w);
-    const int last = max(r.valid, 1) - 1;
-    const uint8_t *k = c.k + (int64_t)page * c.k_page_stride + (int64_t)kvh * c.k_head_stride + (int64_t)at * c.k_key_stride;
-    const uint8_t *v = c.v + (int64_t)page * c.v_page_stride + (int64_t)kvh * c.v_head_stride + (int64_t)at * c.v_key_stride;
-    const uint8_t *ks = c.k_scale + (int64_t)page * c.k_scale_page_stride + (int64_t)kvh * c.k_scale_head_stride + at;
-    const uint8_t *vs = c.v_scale + (int64_t)page * c.v_scale_page_stride + (int64_t)kvh * c.v_scale_head_stride + at;
-    const int key = min(col, last);
-    const uint8_t *row = k + (unsigned)key * (unsigned)c.k_key_stride;
+    k_at = (unsigned)col * (unsigned)c.k_key_stride + piece_bytes(KF, KP.at[0].feats) * quarter;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v_at[j] = (unsigned)(4 * quarter + j) * (unsigned)c.v_key_stride;
+#pragma unroll
+    for (int i = 0; i < KP.n; ++i) ks_at[i] = (unsigned)((KP.at[i].base + KP.at[i].feats * quarter) >> 5) * (unsigned)c.k_scale_group_stride + col;
+#pragma unroll
+    for (int i = 0; i < VP.n; ++i) vs_at[i] = (unsigned)((VP.at[i].base + VP.at[i].feats * col) >> 5) * (unsigned)c.v_scale_group_stride + 4 * quarter;
+  }
+
+  // The codes of a run from its first key's places on.  All sixteen keys lie in the room of their request or page, whether they are there or not:
+  // lengths are looked at when the codes are used.
+  __device__ __forceinline__ void fetch(Run &r, const uint8_t *k, const uint8_t *v, const uint8_t *ks, const uint8_t *vs, int valid, int first) {
+    r.valid = valid;
+    r.first = first;
     int w = 0;
 #pragma unroll
     for (int i = 0; i < KP.n; ++i) {
       constexpr auto P = KP;
-      const int feats = P.at[i].feats, base = P.at[i].base;
-      const int bytes = piece_bytes(KF, feats);
-      const uint8_t *from = row + piece_bytes(KF, base) + bytes * quarter;
-      if (bytes == 16) load_bytes<16>(from, &r.k[w]);
-      else if (bytes == 8) load_bytes<8>(from, &r.k[w]);
-      else load_bytes<4>(from, &r.k[w]);
+      const int bytes = piece_bytes(KF, P.at[i].feats);
+      // the pieces behind the first may be shorter, and a lane's place in them with it
+      const unsigned at = k_at - (unsigned)((piece_bytes(KF, P.at[0].feats) - bytes) * quarter);
+      const uint8_t *from = k + piece_bytes(KF, P.at[i].base) + at;
+      if (bytes == 16) load_bytes<16, kNtK>(from, &r.k[w]);
+      else if (bytes == 8) load_bytes<8, kNtK>(from, &r.k[w]);
+      else load_bytes<4, kNtK>(from, &r.k[w]);
       w += words(bytes);
-      r.ks[i] = ks[(int64_t)((base + feats * quarter) >> 5) * c.k_scale_group_stride + key];
+      r.ks[i] = ks[ks_at[i]];
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint8_t *vrow = v + (unsigned)min(4 * quarter + j, last) * (unsigned)c.v_key_stride;
       w = 0;
 #pragma unroll
       for (int i = 0; i < VP.n; ++i) {
         constexpr auto P = VP;
         const int bytes = piece_bytes(VF, P.at[i].feats);
-        const uint8_t *from = vrow + piece_bytes(VF, P.at[i].base) + bytes * col;
-        if (bytes == 8) load_bytes<8>(from, &r.v[j][w]);
-        else if (bytes == 4) load_bytes<4>(from, &r.v[j][w]);
-        else if (bytes == 2) load_bytes<2>(from, &r.v[j][w]);
-        else load_bytes<1>(from, &r.v[j][w]);
+        const uint8_t *from = v + piece_bytes(VF, P.at[i].base) + (v_at[j] + (unsigned)(bytes * col));
+        if (bytes == 8) load_bytes<8, kNtV>(from, &r.v[j][w]);
+        else if (bytes == 4) load_bytes<4, kNtV>(from, &r.v[j][w]);
+        else if (bytes == 2) load_bytes<2, kNtV>(from, &r.v[j][w]);
+        else load_bytes<1, kNtV>(from, &r.v[j][w]);
         w += words(bytes);
       }
     }
     // four keys' scales at once; the room of a request or page is a multiple of 16
 #pragma unroll
-    for (int i = 0; i < VP.n; ++i) {
-      constexpr auto P = VP;
-      r.vs[i] = *(const unsigned *)(vs + (int64_t)((P.at[i].base + P.at[i].feats * col) >> 5) * c.v_scale_group_stride + 4 * quarter);
-    }
+    for (int i = 0; i < VP.n; ++i) r.vs[i] = *(const unsigned *)(vs + vs_at[i]);
   }
 
   // Raw scores of a run: keys 4 quarter + i of it with this lane's head
@@ -236,19 +240,29 @@ template <typename T, int G, int KF, int VF> struct Token {
     return s;
   }
 
-  // Scores of keys first + 4 quarter + i as exponents of two, -infinity where there is no such key
-  __device__ __forceinline__ void shape(f32x4_t &s, const Run &r, float slope2, int len) {
-    if (p.cap2 != 0.f) {
+  // Scores of keys first + 4 quarter + i as exponents of two, -infinity where there is no such key; raw: all lie where the polynomial of a cap holds
+  __device__ __forceinline__ void shape(f32x4_t &s, const Run &r, float slope2, int len, bool raw) {
+    float factor[4];
+    if (p.cap2 == 0.f) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = cap_any(s[i], p.cap_c, p.cap_most, p.to_cap, p.cap2);
+      for (int i = 0; i < 4; ++i) factor[i] = p.scale2;
+    } else if (raw) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) factor[i] = cap_factor(s[i], p.cap_c);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] *= p.scale2;
+      for (int i = 0; i < 4; ++i) {
+        s[i] = cap_any(s[i], p.cap_c, p.cap_most, p.to_cap, p.cap2);
+        factor[i] = 1.0f;
+      }
     }
     if (p.slopes) {
-      const int far = len - 1 - r.first - 4 * quarter;
+      const float far = slope2 * (float)(len - 1 - r.first - 4 * quarter);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] -= slope2 * (float)(far - i);
+      for (int i = 0; i < 4; ++i) s[i] = fmaf(s[i], factor[i], fmaf(slope2, (float)i, -far));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] *= factor[i];
     }
     if (r.valid < 16) {
 #pragma unroll
@@ -258,8 +272,13 @@ template <typename T, int G, int KF, int VF> struct Token {
 
   __device__ __forceinline__ void step(Run &a, Run &b, float slope2, int len) {
     f32x4_t s0 = scores(a), s1 = scores(b);
-    shape(s0, a, slope2, len);
-    shape(s1, b, slope2, len);
+    bool raw = false;
+    if (p.cap2 != 0.f) {
+      const float far = fmaxf(fmaxf(fmaxf(fabsf(s0[0]), fabsf(s0[1])), fmaxf(fabsf(s0[2]), fabsf(s0[3]))), fmaxf(fmaxf(fabsf(s1[0]), fabsf(s1[1])), fmaxf(fabsf(s1[2]), fabsf(s1[3]))));
+      raw = !__any(!(far <= p.cap_most));  // a NaN stays one by either way
+    }
+    shape(s0, a, slope2, len, raw);
+    shape(s1, b, slope2, len, raw);
     float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
     if (__any(top > m + kFollow)) {
       top = fmaxf(top, __shfl_xor(top, 16));
@@ -316,81 +335,124 @@ template <typename T, int G, int KF, int VF> struct Token {
     }
   }
 
-  // Values of keys that are not there, whose weight is 0, may not be NaN.  Behind the last key that is there its codes were read, under scales of
-  // places that hold anything: a 1 instead of those.  A run without keys was read at a place that may not be seen: zeros.
+  // Values of keys that are not there, whose weight is 0, may not be NaN: zeros under a scale of 1.
   __device__ __forceinline__ void mend(Run &r) {
 #pragma unroll
-    for (int i = 0; i < VP.n; ++i)
+    for (int j = 0; j < 4; ++j) {
+      const bool gone = 4 * quarter + j >= r.valid;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (4 * quarter + j >= r.valid) r.vs[i] = (r.vs[i] & ~(255u << (8 * j))) | 127u << (8 * j);
-    if (r.valid) return;
+      for (int w = 0; w < VW; ++w) r.v[j][w] = gone ? 0u : r.v[j][w];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int w = 0; w < VW; ++w) r.v[j][w] = 0;
+      for (int i = 0; i < VP.n; ++i) r.vs[i] = gone ? (r.vs[i] & ~(255u << (8 * j))) | 127u << (8 * j) : r.vs[i];
+    }
   }
 };
+
+// Where a unit of 16 or 32 keys lies, which is one or two runs: bytes from the tensors' beginnings, its first key, and, of a listed block, how many
+// are there.
+struct __attribute__((aligned(16))) Place {
+  int64_t k, v, ks, vs;
+  int first, valid, pad[2];
+};
+
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)v), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
 
 // One part of a request's keys, of one KV head and up to 16 of its query heads: the waves take pairs of runs in turn, and join what they have in
 // LDS.
 template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(kThreads, 2) k_mx_token(const MxTokenCall p) {
   using Tk = Token<T, G, KF, VF>;
   extern __shared__ char lds[];
-  int4 *places = (int4 *)lds;
-  __shared__ int used;
+  Place *places = (Place *)lds;
   const hyp_mx_cache_t &c = p.m.c;
   const int part = blockIdx.x % p.parts, item = blockIdx.x / p.parts, ht = item % p.head_tiles, pair = item / p.head_tiles;
-  const int b = pair / c.n_kv_heads, kvh = pair % c.n_kv_heads, wave = threadIdx.x >> 6;
-  const int len = mx_len(c, b);
-  const int per = p.m.block_shift - 4;   // log2(runs of a block)
-  const int runs = p.listed ? p.listed << per : (len + 15) >> 4;
-  const int r0 = part * p.runs, n = min(p.runs, runs - r0);
-  if (!p.listed && n <= 0 && part > 0) return;  // the join does not look at it
-  if (threadIdx.x == 0) used = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int r = r0 + i;
-    int4 at = make_int4(b, 0, 0, 0);
-    if (p.listed) {
-      const int block = p.blocks[(int64_t)pair * p.listed + (r >> per)];
-      if (block >= 0 && block <= (len - 1) >> p.m.block_shift && len > 0) {
-        at.w = (block << p.m.block_shift) + ((r & ((1 << per) - 1)) << 4);
-        at.z = mx_clamped(len - at.w, 0, 16);
-      }
-    } else {
-      at.w = r << 4;
-      at.z = min(len - at.w, 16);
-    }
-    if (at.z > 0) {
-      at.y = at.w;
-      if (c.page_table) {
-        at.x = mx_clamped(c.page_table[(int64_t)b * c.pages_per_request + (at.w >> p.m.shift)], 0, c.n_pages - 1);
-        at.y = at.w & (c.page_keys - 1);
-      }
-      atomicMax(&used, i + 1);
-    } else if (c.page_table) {
-      at.x = 0;
-    }
-    places[i] = at;
-  }
-  __syncthreads();
-  const int end = used;                  // runs behind the last one that holds keys are left out
+  const int b = pair / c.n_kv_heads, kvh = pair % c.n_kv_heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int per = p.m.block_shift - p.unit;  // log2(units of a block); a unit has 16 or 32 keys
+  const int unit = 1 << p.unit, u0 = part * p.units;
+  const int len = mx_len(c, b), most = p.listed ? p.listed << per : (int)(((int64_t)c.most + unit - 1) >> p.unit);
   Tk t(p);
-  t.kvh = kvh;
   const int head = ht * 16 + t.col;      // of the group
   const bool there = head < p.G;
   const int qh = kvh * p.G + (there ? head : 0);
   t.load_q(b, qh, there);
+  // all units that the part can have, so that nothing waits for the length; those behind the last one that holds keys are left out below
+  for (int i = threadIdx.x; i < min(p.units, most - u0); i += kThreads) {
+    const int u = u0 + i;
+    Place at = {};
+    at.first = u << p.unit;
+    if (p.listed) {
+      const int block = p.blocks[(int64_t)pair * p.listed + (u >> per)];
+      const bool held = len > 0 && block >= 0 && block <= (len - 1) >> p.m.block_shift;
+      at.first = held ? (block << p.m.block_shift) + ((u & ((1 << per) - 1)) << p.unit) : 0;  // else a place that may be read
+      at.valid = held ? mx_clamped(len - at.first, 0, unit) : 0;
+      if (at.valid == 0) at.first = 0;
+    }
+    int page = b, in = at.first;
+    if (c.page_table) {
+      page = mx_clamped(c.page_table[(int64_t)b * c.pages_per_request + (at.first >> p.m.shift)], 0, c.n_pages - 1);
+      in = at.first & (c.page_keys - 1);
+    }
+    at.k = page * c.k_page_stride + kvh * c.k_head_stride + in * c.k_key_stride;
+    at.v = page * c.v_page_stride + kvh * c.v_head_stride + in * c.v_key_stride;
+    at.ks = page * c.k_scale_page_stride + kvh * c.k_scale_head_stride + in;
+    at.vs = page * c.v_scale_page_stride + kvh * c.v_scale_head_stride + in;
+    places[i] = at;
+  }
+  int end = min(p.units, most - u0);
+  if (!p.listed) {
+    end = min(end, (int)(((int64_t)len + unit - 1) >> p.unit) - u0);
+    if (end <= 0 && part > 0) return;    // the join does not look at it
+  }
+  __syncthreads();
+  t.aim();
   t.clear();
   const float slope2 = p.slopes && there ? p.slopes[qh] * kLog2e : 0.f;
-  const int4 none = make_int4(c.page_table ? 0 : b, 0, 0, 0);
-  auto place = [&](int i) { return i < end ? places[i] : none; };
-  typename Tk::Run a, z;
-  for (int i = 2 * wave; i < end; i += 2 * kWaves) {
-    t.fetch(a, place(i));
-    t.fetch(z, place(i + 1));
-    t.step(a, z, slope2, len);
+  auto fetch = [&](typename Tk::Run &a, typename Tk::Run &z, int i) {
+    const Place at = places[i];
+    const int first = __builtin_amdgcn_readfirstlane(at.first), valid = p.listed ? __builtin_amdgcn_readfirstlane(at.valid) : len - first;
+    const uint8_t *k = c.k + uniform64(at.k), *v = c.v + uniform64(at.v), *ks = c.k_scale + uniform64(at.ks), *vs = c.v_scale + uniform64(at.vs);
+    t.fetch(a, k, v, ks, vs, valid, first);
+    if (p.unit == 5) {
+      t.fetch(z, k + 16 * c.k_key_stride, v + 16 * c.v_key_stride, ks + 16, vs + 16, valid - 16, first + 16);
+    } else {
+      const bool more = i + 1 < end;
+      const Place of = places[more ? i + 1 : i];
+      const int from = __builtin_amdgcn_readfirstlane(of.first);
+      t.fetch(z, c.k + uniform64(of.k), c.v + uniform64(of.v), c.k_scale + uniform64(of.ks), c.v_scale + uniform64(of.vs),
+              !more ? 0 : p.listed ? __builtin_amdgcn_readfirstlane(of.valid) : len - from, from);
+    }
+  };
+  const int each = p.unit == 5 ? 1 : 2, STEP = kWaves * each;
+  int i = wave * each;
+  if constexpr (G <= 4) {
+    // the next pair of runs is on its way while one is worked on
+    typename Tk::Run a[2], z[2];
+    if (i < end) {
+      fetch(a[0], z[0], i);
+      for (;;) {
+        if (i + STEP >= end) {
+          t.step(a[0], z[0], slope2, len);
+          break;
+        }
+        fetch(a[1], z[1], i + STEP);
+        t.step(a[0], z[0], slope2, len);
+        i += 2 * STEP;
+        if (i >= end) {
+          t.step(a[1], z[1], slope2, len);
+          break;
+        }
+        fetch(a[0], z[0], i);
+        t.step(a[1], z[1], slope2, len);
+      }
+    }
+  } else {
+    for (; i < end; i += STEP) {
+      typename Tk::Run a, z;
+      fetch(a, z, i);
+      t.step(a, z, slope2, len);
+    }
   }
   // join the waves: O^T is features x heads, lane (head, quarter) has features base + (4 quarter + r) feats + x
   t.l += __shfl_xor(t.l, 16);
@@ -457,7 +519,7 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
 }
 
 template <int G, typename T> constexpr int token_lds(int heads) {
-  const int joined = 2 * kWaves * 16 * 4 + kWaves * heads * (32 * G + 4) * 4, places = kMxMostRuns * 16;
+  const int joined = 2 * kWaves * 16 * 4 + kWaves * heads * (32 * G + 4) * 4, places = kMxMostUnits * (int)sizeof(Place);
   return joined > places ? joined : places;
 }
 
