@@ -126,7 +126,7 @@ HYP_API hyp_status_t mx_read(const hyp_mx_cache_t *cache, const int32_t *first, 
 /* For every request and KV head the blocks that a row should read: of at most `keep` blocks the first `sink`
  * and the newest `recent` always, then those of the largest score, of equal scores the first; all where a
  * request holds no more than keep.  For query head h of the group and block i
- *   score(h, i) = sum over features f of (q_f >= 0 ? q_f * hi_f : q_f * lo_f),
+ *   score(h, i) = sum over features f of max(q_f, 0) * hi_f + min(q_f, 0) * lo_f,
  * which no <q, k> of the block passes; a KV head's is the largest of its query heads.  Scores are formed in
  * 64 bits; one that is NaN counts as larger than any number.  Distances (slopes) are not looked at, and a
  * cap, which keeps the order, has no part in it.

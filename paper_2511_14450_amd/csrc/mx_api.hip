@@ -222,12 +222,11 @@ hyp_status_t mx_select(const hyp_mx_cache_t *cache, const hyp_mx_q_t *q, int32_t
     const int64_t pairs = (int64_t)c.n_requests * c.n_kv_heads;
     if (bytes) {
       check_launch(pairs, 1024);
-      check_launch(pairs * ((p.most_blocks + kMxScoreBlocks - 1) / kMxScoreBlocks), 256);
+      check_launch(pairs * mx_score_tiles(p.most_blocks, mx_score_turns(pairs, p.most_blocks)), 256);
     } else {
       check_launch(pairs, 256);
     }
-    p.wide_q = pieces(q->q, es_of(q->dtype), c.head_dim, q->q_row_stride, q->q_head_stride);
-    p.wide_bound = pieces(c.lo, 2, c.head_dim, c.bound_page_stride, c.bound_head_stride, c.bound_block_stride) && aligned(c.hi, 16);
+    p.wide = pieces(q->q, es_of(q->dtype), c.head_dim, q->q_row_stride, q->q_head_stride) && pieces(c.lo, 2, c.head_dim, c.bound_page_stride, c.bound_head_stride, c.bound_block_stride) && aligned(c.hi, 16);
     const hipStream_t s = (hipStream_t)hip_stream;
     run(q->dtype == HYP_BF16 ? mx_select<bf16_t>(p, s) : mx_select<float>(p, s));
   });

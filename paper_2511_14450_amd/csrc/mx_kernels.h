@@ -35,7 +35,7 @@ struct MxSelectCall {
   int *blocks;
   int most_blocks;
   unsigned long long *order;  // [n_requests][n_kv_heads][most_blocks]
-  int wide_q, wide_bound;
+  int wide;                   // eight features of a row and of a bound are whole 16-byte pieces
 };
 
 struct MxTokenCall {

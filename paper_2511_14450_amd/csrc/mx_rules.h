@@ -14,8 +14,16 @@ constexpr int kMxPlainBlock = 64;    // mx_write: keys of a tile where the cache
 inline int64_t mx_write_tiles(int64_t rows, int64_t requests, int64_t block, bool one_each) { return one_each ? requests : rows / block + 2 * requests; }
 
 // mx_select: in one launch up to so many blocks of a request, or where all are kept.
-constexpr int kMxSmallBlocks = 256, kMxScoreBlocks = 64;  // else blocks of a workgroup that forms scores
+constexpr int kMxSmallBlocks = 256;
 inline bool mx_select_once(int blocks, int keep) { return blocks <= kMxSmallBlocks || blocks <= keep; }
+// Else scores are formed by workgroups of 64 blocks once to four times: a row is converted once for all of them, but there have to be two workgroups
+// a CU.
+inline int mx_score_turns(int64_t pairs, int64_t blocks) {
+  int turns = 4;
+  while (turns > 1 && pairs * ((blocks + 64 * turns - 1) / (64 * turns)) < 512) turns /= 2;
+  return turns;
+}
+inline int mx_score_tiles(int64_t blocks, int turns) { return (int)((blocks + 64 * turns - 1) / (64 * turns)); }
 
 // mx_token: units of 32 keys, or of 16 where pages or listed blocks are so short, of a part, and parts of a request.
 constexpr int kMxMostUnits = 256;    // of a part: their places lie in LDS

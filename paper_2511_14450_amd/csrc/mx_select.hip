@@ -19,125 +19,143 @@ __device__ __forceinline__ u64 order_of(double x) {
   return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
 }
 
-template <int X> __device__ __forceinline__ double row_xor(double v) {  // of the 16 lanes of a row
-  const u64 u = (u64)__double_as_longlong(v);
-  constexpr int ctrl = X == 1 ? 0xb1 : X == 2 ? 0x4e : X == 4 ? 0x141 : 0x128;  // quad_perm, quad_perm, row_half_mirror, row_ror:8
+template <int X> __device__ __forceinline__ u64 quad_xor(u64 u) {  // of the four lanes of a quad
+  constexpr int ctrl = X == 1 ? 0xb1 : 0x4e;
   const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, 0xf, 0xf, true);
   const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, 0xf, 0xf, true);
-  return __longlong_as_double((long long)((u64)hi << 32 | lo));
+  return (u64)hi << 32 | lo;
 }
 
-template <typename T> __device__ __forceinline__ void load_q(const MxSelectCall &p, int b, int head, int f, double (&x)[8]) {
-  const int d = p.m.c.head_dim;
-  const T *q = (const T *)p.q.q + b * p.q.q_row_stride + head * p.q.q_head_stride;
-  if (p.wide_q && f < d) {
-    if constexpr (sizeof(T) == 2) {
-      const u16x8_t v = *(const u16x8_t *)(q + f);
+// Features f .. f + 7 of a row of d as 64 bits, zeros from d on.  WIDE: whole pieces of 16 bytes; no branch is in the way of requesting several.
+template <typename T, bool WIDE> struct Eight {
+  static constexpr int N = sizeof(T) / 2;
+  uint4 w[N];
+  __device__ __forceinline__ void load(const T *row, int f, int d) {
+    if constexpr (WIDE) {
+      const uint4 *at = (const uint4 *)(row + min(f, d - 8));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (double)bf16_to_f32(v.v[i]);
+      for (int i = 0; i < N; ++i) w[i] = at[i];
     } else {
+      T x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (double)q[f + i];
+      for (int i = 0; i < 8; ++i) x[i] = f + i < d ? row[f + i] : (T)0;
+      __builtin_memcpy(w, x, sizeof(x));
     }
-    return;
   }
+  __device__ __forceinline__ void get(int f, int d, double (&x)[8]) const {
+    T y[8];
+    __builtin_memcpy(y, w, sizeof(y));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = f + i < d ? (double)load_f32(q + f + i) : 0.0;
-}
+    for (int i = 0; i < 8; ++i) x[i] = !WIDE || f < d ? (double)load_f32(y + i) : 0.0;
+  }
+};
 
-// Features f .. f + 7 of a block's bound, two a word, as they lie in memory
-__device__ __forceinline__ uint4 load_bound(const bf16_t *row, int f, int d, bool wide) {
-  if (wide && f < d) return *(const uint4 *)(row + f);
+// Features f .. f + 7 of a block's bound, two a word, as they lie in memory, zeros from d on
+template <bool WIDE> __device__ __forceinline__ uint4 load_bound(const bf16_t *row, int f, int d) {
+  if constexpr (WIDE) return *(const uint4 *)(row + min(f, d - 8));
   unsigned w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = (f + 2 * i < d ? row[f + 2 * i] : 0u) | (f + 2 * i + 1 < d ? row[f + 2 * i + 1] : 0u) << 16;
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ unsigned word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-
-__device__ __forceinline__ int64_t bound_at(const MxSelectCall &p, int b, int kvh, int i) {
-  const hyp_mx_cache_t &c = p.m.c;
-  if (!c.page_table) return (int64_t)b * c.bound_page_stride + kvh * c.bound_head_stride + i * c.bound_block_stride;
-  const int s = p.m.shift - p.m.block_shift;  // log2(blocks of a page)
-  const int page = mx_clamped(c.page_table[(int64_t)b * c.pages_per_request + (i >> s)], 0, c.n_pages - 1);
-  return (int64_t)page * c.bound_page_stride + kvh * c.bound_head_stride + (i & ((1 << s) - 1)) * c.bound_block_stride;
+__device__ __forceinline__ double element(const uint4 &v, int i, bool there) {
+  const unsigned w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w, x = i & 1 ? w & 0xffff0000u : w << 16;
+  return (double)__uint_as_float(there ? x : 0u);
 }
 
-// Order of the scores of blocks i0, i0 + step, ... below i1 of one request and KV head: 16 lanes a block, eight features a lane (PIECES times),
-// kBatch blocks at a time, whose bounds are all requested before the first is used.  What is formed of 8-bit products in 64 bits is exact for all
-// but wide spreads of sizes, so that the choice does not hang on the order of the sums.
-template <typename T, int PIECES, typename Put> __device__ __forceinline__ void score_blocks(const MxSelectCall &p, int b, int kvh, int i0, int i1, int step, Put &&put) {
-  constexpr int kBatch = 4 / PIECES;
+// Order of the scores of blocks first + 64 t + 16 wave + 0..15, t < kTurns, as far as `end`, of one request and KV head.  The sums are formed in 64
+// bits, for which products of bf16 numbers are exact for all but wide spreads of sizes, so that the choice does not hang on their order.
+// The vector unit has neither the time for that (a conversion of a float takes four ordinary instructions': 22 us for 64 caches of up to 2048
+// blocks of 128 features) nor for the sums over lanes; the matrix unit's 4 x 4 x 4 product does both: 16 blocks on the M axis of its four
+// batches, 4 heads on the N axis, lane l holds blocks l % 16 and heads l % 4 in four pieces of features, l / 16 of them, and gets the score of
+// block 4 (l / 4 % 4) + l / 16 with head l % 4.  N: pieces of eight features of a lane at a time.
+constexpr int kTurns = 4;
+template <typename T, int N, bool WIDE, typename Put> __device__ __forceinline__ void score_blocks(const MxSelectCall &p, int b, int kvh, int first, int turns, int end, Put &&put) {
   const hyp_mx_cache_t &c = p.m.c;
-  const int lane = threadIdx.x & 15, d = c.head_dim, group = p.q.n_q_heads / c.n_kv_heads;
+  const int lane = threadIdx.x & 63, chunk = lane >> 4, d = c.head_dim, group = p.q.n_q_heads / c.n_kv_heads;
+  first += 16 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (first >= end) return;
   const bf16_t *lo = (const bf16_t *)c.lo, *hi = (const bf16_t *)c.hi;
+  int page[kTurns], in[kTurns];
+  int64_t at[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    page[t] = b;
+    in[t] = min(first + 64 * min(t, turns - 1) + (lane & 15), end - 1);
+  }
+  if (c.page_table) {
+    const int s = p.m.shift - p.m.block_shift;  // log2(blocks of a page)
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) page[t] = c.page_table[(int64_t)b * c.pages_per_request + (in[t] >> s)];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+      page[t] = mx_clamped(page[t], 0, c.n_pages - 1);
+      in[t] &= (1 << s) - 1;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) at[t] = page[t] * c.bound_page_stride + kvh * c.bound_head_stride + in[t] * c.bound_block_stride;
   for (int g0 = 0; g0 < group; g0 += kHeads) {
-    double q[kHeads][PIECES][8];
-    unsigned up[kHeads][PIECES][4];  // where a feature's largest number counts, else its least: two a word, as the bounds
+    const T *row = (const T *)p.q.q + b * p.q.q_row_stride + (kvh * group + min(g0 + (lane & 3), group - 1)) * p.q.q_head_stride;
+    double up[kTurns], down[kTurns];     // sums over features whose largest numbers count, and whose least do
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
+    for (int t = 0; t < kTurns; ++t) up[t] = down[t] = 0.0;
+    for (int from = 0; from < d; from += 32 * N) {
+      Eight<T, WIDE> raw[N];
+      uint4 l[2][N], u[2][N];
+      auto place = [&](int n) { return from + 32 * n + 8 * chunk; };
+      auto request = [&](int t) {
 #pragma unroll
-      for (int x = 0; x < PIECES; ++x) {
-        load_q<T>(p, b, kvh * group + min(g0 + h, group - 1), x * 128 + lane * 8, q[h][x]);
+        for (int n = 0; n < N; ++n) {
+          u[t & 1][n] = load_bound<WIDE>(hi + at[t], place(n), d);
+          l[t & 1][n] = load_bound<WIDE>(lo + at[t], place(n), d);
+        }
+      };
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          up[h][x][k] = (q[h][x][2 * k] >= 0.0 ? 0xffffu : 0u) | (q[h][x][2 * k + 1] >= 0.0 ? 0xffff0000u : 0u);
+      for (int n = 0; n < N; ++n) raw[n].load(row, place(n), d);
+      request(0);
+      double qu[N][8], ql[N][8];         // max(q, 0) and min(q, 0)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        double q[8];
+        raw[n].get(place(n), d, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          qu[n][e] = q[e] < 0.0 ? 0.0 : q[e];  // NaN stays one in both
+          ql[n][e] = q[e] > 0.0 ? 0.0 : q[e];
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        if (t > 0 && (t >= turns || first + 64 * t >= end)) break;
+        if (t + 1 < kTurns) request(t + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            up[t] = __builtin_amdgcn_mfma_f64_4x4x4f64(element(u[t & 1][n], e, place(n) < d), qu[n][e], up[t], 0, 0, 0);
+            down[t] = __builtin_amdgcn_mfma_f64_4x4x4f64(element(l[t & 1][n], e, place(n) < d), ql[n][e], down[t], 0, 0, 0);
+          }
       }
     }
-    for (int first = i0; first < i1; first += step * kBatch) {
-      int64_t at[kBatch];
 #pragma unroll
-      for (int n = 0; n < kBatch; ++n) at[n] = bound_at(p, b, kvh, min(first + n * step, i1 - 1));
-      double sum[kBatch][kHeads];
-#pragma unroll
-      for (int n = 0; n < kBatch; ++n)
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h) sum[n][h] = 0.0;
-#pragma unroll
-      for (int x = 0; x < PIECES; ++x) {
-        uint4 l[kBatch], u[kBatch];
-#pragma unroll
-        for (int n = 0; n < kBatch; ++n) {
-          l[n] = load_bound(lo + at[n], x * 128 + lane * 8, d, p.wide_bound);
-          u[n] = load_bound(hi + at[n], x * 128 + lane * 8, d, p.wide_bound);
-        }
-#pragma unroll
-        for (int n = 0; n < kBatch; ++n)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int h = 0; h < kHeads; ++h) {
-              const unsigned m = up[h][x][k], w = (word_of(u[n], k) & m) | (word_of(l[n], k) & ~m);
-              sum[n][h] = fma(q[h][x][2 * k], (double)__uint_as_float(w << 16), sum[n][h]);
-              sum[n][h] = fma(q[h][x][2 * k + 1], (double)__uint_as_float(w & 0xffff0000u), sum[n][h]);
-            }
-      }
-#pragma unroll
-      for (int n = 0; n < kBatch; ++n) {
-        u64 best = 0;
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-          double v = sum[n][h];
-          v += row_xor<1>(v);
-          v += row_xor<2>(v);
-          v += row_xor<4>(v);
-          v += row_xor<8>(v);
-          best = max(best, order_of(v));
-        }
-        const int i = first + n * step;
-        if (lane == 0 && i < i1) put(i, best, g0 > 0);
-      }
+    for (int t = 0; t < kTurns; ++t) {
+      u64 best = order_of(up[t] + down[t]);
+      best = max(best, quad_xor<1>(best));
+      best = max(best, quad_xor<2>(best));
+      const int i = first + 64 * t + 4 * ((lane >> 2) & 3) + chunk;
+      if ((lane & 3) == 0 && t < turns && i < end) put(i, best, g0 > 0);
     }
   }
 }
 
-template <typename T, int PIECES> __global__ void __launch_bounds__(kThreads) k_mx_scores(const MxSelectCall p, int tiles, int tile_blocks) {
+template <typename T, int N, bool WIDE> __global__ void __launch_bounds__(kThreads, 2) k_mx_scores(const MxSelectCall p, int tiles, int turns) {
   const int tile = blockIdx.x % tiles, pair = blockIdx.x / tiles, b = pair / p.m.c.n_kv_heads, kvh = pair % p.m.c.n_kv_heads;
   const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
   if (count <= p.keep) return;
-  const int i0 = tile * tile_blocks, i1 = min(count, i0 + tile_blocks);
   u64 *order = p.order + (int64_t)pair * p.most_blocks;
-  score_blocks<T, PIECES>(p, b, kvh, i0 + (threadIdx.x >> 4), i1, kThreads / 16, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
+  score_blocks<T, N, WIDE>(p, b, kvh, tile * 64 * turns, turns, min(count, (tile + 1) * 64 * turns), [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
 }
 
 // sum of v over the threads before this one, and over all; scratch: one int a wave
@@ -319,7 +337,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_mx_choose(const MxSelectCall
 }
 
 // The same for requests of up to 256 blocks, scores and choice in one launch: a block is taken if fewer than `keep` come before it.
-template <typename T, int PIECES> __global__ void __launch_bounds__(kThreads) k_mx_select_small(const MxSelectCall p) {
+template <typename T, int N, bool WIDE> __global__ void __launch_bounds__(kThreads, 2) k_mx_select_small(const MxSelectCall p) {
   __shared__ u64 order[kMxSmallBlocks];
   __shared__ int scratch[kThreads / 64];
   const int pair = blockIdx.x, b = pair / p.m.c.n_kv_heads, kvh = pair % p.m.c.n_kv_heads, tid = threadIdx.x, K = p.keep;
@@ -329,7 +347,7 @@ template <typename T, int PIECES> __global__ void __launch_bounds__(kThreads) k_
     for (int r = tid; r < K; r += kThreads) out[r] = r < count ? r : -1;
     return;
   }
-  score_blocks<T, PIECES>(p, b, kvh, tid >> 4, count, kThreads / 16, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
+  score_blocks<T, N, WIDE>(p, b, kvh, 0, kTurns, count, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
   __syncthreads();
   if (tid >= count) order[tid] = 0;
   else if (tid < p.sink || tid >= count - p.recent) order[tid] = ~0ull;
@@ -346,14 +364,14 @@ template <typename T, int PIECES> __global__ void __launch_bounds__(kThreads) k_
   if (taken) out[at] = tid;
 }
 
-template <typename T, int PIECES> hipError_t select(const MxSelectCall &p, hipStream_t s) {
+template <typename T, int N, bool WIDE> hipError_t select(const MxSelectCall &p, hipStream_t s) {
   const unsigned pairs = (unsigned)p.m.c.n_requests * p.m.c.n_kv_heads;
   if (mx_select_once(p.most_blocks, p.keep)) {
-    k_mx_select_small<T, PIECES><<<pairs, kThreads, 0, s>>>(p);
+    k_mx_select_small<T, N, WIDE><<<pairs, kThreads, 0, s>>>(p);
     return hipGetLastError();
   }
-  const int tiles = (p.most_blocks + kMxScoreBlocks - 1) / kMxScoreBlocks;
-  k_mx_scores<T, PIECES><<<pairs * tiles, kThreads, 0, s>>>(p, tiles, kMxScoreBlocks);
+  const int turns = mx_score_turns(pairs, p.most_blocks), tiles = mx_score_tiles(p.most_blocks, turns);
+  k_mx_scores<T, N, WIDE><<<pairs * tiles, kThreads, 0, s>>>(p, tiles, turns);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;  // the choice goes by the scores
   k_mx_choose<<<pairs, kSelectThreads, 0, s>>>(p);
@@ -363,7 +381,8 @@ template <typename T, int PIECES> hipError_t select(const MxSelectCall &p, hipSt
 }  // namespace
 
 template <typename T> hipError_t mx_select(const MxSelectCall &p, hipStream_t s) {
-  return p.m.c.head_dim <= 128 ? select<T, 1>(p, s) : select<T, 2>(p, s);
+  if (p.wide) return p.m.c.head_dim <= 64 ? select<T, 2, true>(p, s) : select<T, 4, true>(p, s);
+  return select<T, 2, false>(p, s);
 }
 
 template hipError_t mx_select<float>(const MxSelectCall &, hipStream_t);

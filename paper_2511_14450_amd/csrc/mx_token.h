@@ -120,43 +120,70 @@ template <typename T, int G, int KF, int VF> struct Token {
 
   __device__ __forceinline__ Token(const MxTokenCall &call) : p(call), lane(threadIdx.x & 63), col(lane & 15), quarter(lane >> 4) {}
 
+  // First feature of the steps of K's pieces: base + feats * quarter
+  struct Steps {
+    int base[G] = {}, feats[G] = {};
+    constexpr Steps() {
+      int s = 0;
+      for (int i = 0; i < KP.n; ++i)
+        for (int x = 0; x < KP.at[i].feats; x += 8, ++s) {
+          base[s] = KP.at[i].base + x;
+          feats[s] = KP.at[i].feats;
+        }
+    }
+  };
+  __device__ __forceinline__ int feature(int s) const {
+    constexpr Steps S{};
+    return S.base[s] + S.feats[s] * quarter;
+  }
+
   // Row of head `head` (of q), as the N operand of the steps of K's pieces; zeros where there is no such head
   __device__ __forceinline__ void load_q(int b, int head, bool there) {
     const T *row = (const T *)p.q.q + b * p.q.q_row_stride + head * p.q.q_head_stride;
     const int d = p.m.c.head_dim;
-    int step = 0;
+    constexpr int W = 2 * sizeof(T);     // words of eight features
+    unsigned x[G][W];
+    if (p.wide_q) {  // all pieces are requested before one is looked at
 #pragma unroll
-    for (int i = 0; i < KP.n; ++i) {
+      for (int s = 0; s < G; ++s) {
+        const uint4 *from = (const uint4 *)(row + min(feature(s), d - 8));
 #pragma unroll
-      for (int s = 0; s < KP.at[i].feats / 8; ++s, ++step) {
-        const int f = KP.at[i].base + KP.at[i].feats * quarter + 8 * s;
-        float x[8];
+        for (int i = 0; i < W / 4; ++i) {
+          const uint4 v = from[i];
+          x[s][4 * i] = v.x; x[s][4 * i + 1] = v.y; x[s][4 * i + 2] = v.z; x[s][4 * i + 3] = v.w;
+        }
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (there) {
-          if (p.wide_q && f < d) {
-            if constexpr (sizeof(T) == 2) {
-              const u16x8_t v = *(const u16x8_t *)(row + f);
+      for (int s = 0; s < G; ++s)
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = bf16_to_f32(v.v[e]);
-            } else {
-              const f32x4_t a = *(const f32x4_t *)(row + f), z = *(const f32x4_t *)(row + f + 4);
+        for (int i = 0; i < W; ++i) x[s][i] = there && feature(s) < d ? x[s][i] : 0u;
+    } else {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                x[e] = a[e];
-                x[4 + e] = z[e];
-              }
-            }
-          } else {
+      for (int s = 0; s < G; ++s)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (f + e < d) x[e] = load_f32(row + f + e);
+        for (int i = 0; i < W; ++i) {
+          x[s][i] = 0;
+#pragma unroll
+          for (int e = 0; e < 4 / (int)sizeof(T); ++e) {
+            const int f = feature(s) + i * 4 / (int)sizeof(T) + e;
+            unsigned v = 0;
+            __builtin_memcpy(&v, row + min(f, d - 1), sizeof(T));
+            x[s][i] |= (there && f < d ? v : 0u) << (16 * e);
           }
         }
-        bf16x8_t part[QP];
-        split8<QP>(x, part);
+    }
 #pragma unroll
-        for (int t = 0; t < QP; ++t) q[t][step] = part[t];
+    for (int s = 0; s < G; ++s) {
+      if constexpr (QP == 1) {
+        q[0][s] = as_bf16x8(x[s]);
+      } else {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __uint_as_float(x[s][e]);
+        bf16x8_t part[QP];
+        split8<QP>(y, part);
+#pragma unroll
+        for (int t = 0; t < QP; ++t) q[t][s] = part[t];
       }
     }
   }
@@ -362,7 +389,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 
 // One part of a request's keys, of one KV head and up to 16 of its query heads: the waves take pairs of runs in turn, and join what they have in
 // LDS.
-template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(kThreads, 2) k_mx_token(const MxTokenCall p) {
+template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && G > 6 ? 1 : 2) k_mx_token(const MxTokenCall p) {
   using Tk = Token<T, G, KF, VF>;
   extern __shared__ char lds[];
   Place *places = (Place *)lds;
@@ -426,7 +453,7 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
   };
   const int each = p.unit == 5 ? 1 : 2, STEP = kWaves * each;
   int i = wave * each;
-  if constexpr (G <= 4) {
+  if constexpr (G <= (sizeof(T) == 4 ? 3 : 4)) {
     // the next pair of runs is on its way while one is worked on
     typename Tk::Run a[2], z[2];
     if (i < end) {

@@ -94,7 +94,7 @@ def select(q, lo, hi, held, block, keep, sink, recent):
     for i in range(count):
         best = None
         for row in q.double():
-            s = float(torch.where(row >= 0, row * hi[i].double(), row * lo[i].double()).sum())
+            s = float((row.clamp(min=0) * hi[i].double() + row.clamp(max=0) * lo[i].double()).sum())  # clamp keeps a NaN
             s = (1, 0.0) if math.isnan(s) else (0, s)
             best = s if best is None or s > best else best
         score.append(best)
