@@ -149,10 +149,10 @@ hyp_status_t mx_write(const hyp_mx_cache_t *cache, const hyp_mx_rows_t *rows, vo
     }
     if (r.n_rows == 0) return;
     p.r = r;
-    const int block = c.lo ? c.block_keys : kMxPlainBlock;
+    const int block = c.lo ? c.block_keys : c.page_table ? std::min(c.page_keys, kMxPlainBlock) : kMxPlainBlock;  // a tile lies in one page
     p.block_shift = log2_of(block);
     const int64_t tiles = mx_write_tiles(r.n_rows, c.n_requests, block, !r.q_start);
-    check_launch(tiles * heads, 256);
+    check_launch(tiles * heads, 512);
     p.tiles = (int)tiles;
     const int d = c.head_dim;
     p.wide = pieces(r.k, es, d, r.k_row_stride, r.k_head_stride) && pieces(r.v, es, d, r.v_row_stride, r.v_head_stride) &&
