@@ -1,0 +1,170 @@
+"""Decoder blocks over long contexts whose caches take 8 or 4 bits a number, and whose tokens read them whole or in selected blocks of keys.
+
+What the four operators of mx.py do in one block:
+
+    prompt   mx_write    the keys and values of a prompt's next chunk become codes, and move the bounds of their blocks of keys along
+             mx_read     what its request holds by then, for attn_prompt: a row sees the same numbers as any later token
+    token    mx_write    one key and value a request
+             mx_select   the blocks of keys that can score highest with the token (read_blocks > 0)
+             mx_token    attention over those, or over all
+
+A context may also come from a stage that ran the prompts (`adopt`): its caches are exported and written as codes.
+
+    python -m paper_2511_14450_amd.longctx --requests 8 --prompt 16384 --generate 64 --read-blocks 64
+"""
+from __future__ import annotations
+
+import argparse
+import json
+import time
+from typing import Dict, Sequence
+
+import torch
+
+from . import attn, binding, mx
+from .shared import BlockMath
+
+
+class LongBlocks(BlockMath):
+    """Blocks over n_requests requests of up to `most` keys.
+
+    k_format, v_format  "e4m3" (8 bits) or "e2m1" (4)
+    read_blocks  blocks of block_keys keys that a token reads for each KV head, the first `sink` and the newest `recent` always; 0: all keys
+    page_keys    keys in pages of so many (0: slabs); the page table, the same for all blocks, is the attribute page_table
+    """
+
+    def __init__(self, shape, layers: Sequence[Dict[str, torch.Tensor]], n_requests: int, most: int, k_format: str = "e4m3", v_format: str = "e4m3",
+                 read_blocks: int = 0, block_keys: int = 64, sink: int = 1, recent: int = 4, page_keys: int = 0):
+        if read_blocks < 0 or sink < 0 or recent < 0 or (read_blocks and sink + recent > read_blocks):
+            raise ValueError("need sink + recent within read_blocks, none of them negative")
+        if n_requests < 1 or most < 1:
+            raise ValueError("need n_requests and most of at least 1")
+        super().__init__(shape, layers)
+        self.n, self.most, self.read_blocks, self.sink, self.recent = n_requests, most, read_blocks, sink, recent
+        self.lens = torch.zeros(n_requests, dtype=torch.int32, device="cuda")
+        self.page_table = None
+        self.caches = []
+        for _ in self.layers:
+            self.caches.append(mx.MxCache.allocate(n_requests, shape.n_kv_heads, most, shape.head_dim, k_format, v_format, block_keys if read_blocks else 0, page_keys,
+                                                   lens=self.lens, page_table=self.page_table))
+            self.page_table = self.caches[0].page_table
+        self.held = [0] * n_requests   # what lens counts, on the host
+
+    def _grow(self, counts: Sequence[int]) -> None:
+        if len(counts) != self.n or min(counts) < 0:
+            raise ValueError("need a number of new tokens for every request")
+        if any(h + c > self.most for h, c in zip(self.held, counts)):
+            raise ValueError(f"a request would hold more than {self.most} keys")
+        self.held = [h + c for h, c in zip(self.held, counts)]
+
+    def reset(self) -> None:
+        """All requests start anew."""
+        self.held = [0] * self.n
+        self.lens.zero_()
+
+    def prefill(self, hidden: torch.Tensor, seq_lens: Sequence[int]) -> torch.Tensor:
+        """Hidden states [sum(seq_lens), H] of the requests' prompts, or of their next chunks (0 tokens of some, if any), through the blocks."""
+        if hidden.shape[0] != sum(seq_lens):
+            raise ValueError("need as many rows as seq_lens say")
+        past = list(self.held)
+        self._grow(seq_lens)
+        self.lens.copy_(torch.tensor(self.held, dtype=torch.int32))
+        s, keys = self.shape, max(self.held)
+        if hidden.shape[0] == 0:
+            return hidden
+        start = torch.tensor([sum(seq_lens[:i]) for i in range(self.n + 1)], dtype=torch.int32).cuda()
+        turn = self._turn(torch.cat([torch.arange(p, p + n) for p, n in zip(past, seq_lens)]).cuda())
+        # room for what the requests hold, which all blocks use in turn
+        k = torch.empty((self.n, s.n_kv_heads, keys, s.head_dim), dtype=hidden.dtype, device="cuda")
+        v = torch.empty_like(k)
+        whole = attn.AttnCache(k, v, self.lens)
+        x = hidden
+        for w, cache in zip(self.layers, self.caches):
+            q, new_k, new_v = self._qkv(w, x, turn)
+            mx.mx_write(cache, new_k, new_v, q_start=start)
+            mx.mx_read(cache, k, v)
+            out, _ = attn.attn_prompt(whole, self.rule, q, start)
+            x = self._rest(w, x, out)
+        return x
+
+    def decode_step(self, hidden: torch.Tensor) -> torch.Tensor:
+        """The next token of every request, [n_requests, H]."""
+        if hidden.shape[0] != self.n:
+            raise ValueError("need one row for each request")
+        turn, x = self._turn(self.lens), hidden
+        self._grow([1] * self.n)
+        self.lens += 1
+        for w, cache in zip(self.layers, self.caches):
+            q, k, v = self._qkv(w, x, turn)
+            mx.mx_write(cache, k, v)
+            blocks = mx.mx_select(cache, q, self.read_blocks, self.sink, self.recent) if self.read_blocks else None
+            out, _ = mx.mx_token(cache, self.rule, q, blocks=blocks)
+            x = self._rest(w, x, out)
+        return x
+
+    def adopt(self, stage: binding.Stage, l_start: int, l_end: int) -> None:
+        """The contexts of a stage's first n_requests requests, of the blocks [l_start, l_end) of the stage, which are these blocks; what was held is dropped."""
+        if l_end - l_start != len(self.layers):
+            raise ValueError("need as many blocks of the stage as there are here")
+        lens = [binding.stage_context_len(stage, b) for b in range(self.n)]
+        self.reset()
+        self._grow(lens)
+        self.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        s = self.shape
+        start = torch.tensor([sum(lens[:i]) for i in range(self.n + 1)], dtype=torch.int32).cuda()
+        for l, cache in zip(range(l_start, l_end), self.caches):
+            rows = [torch.cat(t).view(-1, s.n_kv_heads, s.head_dim) for t in zip(*(stage.export_kv(l, b) for b in range(self.n)))]
+            mx.mx_write(cache, *rows, q_start=start)
+
+    def cache_bytes(self) -> int:
+        return sum(t.numel() * t.element_size() for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale, c.lo, c.hi) if t is not None)
+
+
+def main():
+    from .chain import MODELS, _Shape, _synthetic_layer
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--model", choices=sorted(MODELS), default="phi3_medium")
+    ap.add_argument("--blocks", type=int, default=2)
+    ap.add_argument("--requests", type=int, default=8)
+    ap.add_argument("--prompt", type=int, default=16384, help="tokens of each request's prompt")
+    ap.add_argument("--chunk", type=int, default=4096, help="of which so many at a time")
+    ap.add_argument("--generate", type=int, default=64)
+    ap.add_argument("--k-format", choices=sorted(mx.MX_FORMATS), default="e4m3")
+    ap.add_argument("--v-format", choices=sorted(mx.MX_FORMATS), default="e4m3")
+    ap.add_argument("--read-blocks", type=int, default=0, help="blocks of 64 keys that a token reads (0: all)")
+    ap.add_argument("--page-keys", type=int, default=0)
+    ap.add_argument("--seed", type=int, default=251114450)
+    a = ap.parse_args()
+    shape = _Shape(MODELS[a.model])
+    make = _synthetic_layer(shape, a.seed)
+    layers = [make(l) for l in range(a.blocks)]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(a.seed + 13)
+    draw = lambda rows: torch.randn((rows, shape.hidden), generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    blocks = LongBlocks(shape, layers, a.requests, a.prompt + a.generate, a.k_format, a.v_format, a.read_blocks, page_keys=a.page_keys)
+    chunks = [min(a.chunk, a.prompt - at) for at in range(0, a.prompt, a.chunk)]
+    inputs = [draw(a.requests * n) for n in chunks]
+
+    def run(steps):
+        blocks.reset()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for n, x in zip(chunks, inputs):
+            h = blocks.prefill(x, [n] * a.requests)
+        h = h[torch.arange(1, a.requests + 1, device="cuda") * chunks[-1] - 1]
+        torch.cuda.synchronize()
+        t1 = time.perf_counter()
+        for _ in range(steps):
+            h = blocks.decode_step(h)
+        torch.cuda.synchronize()
+        return t1 - t0, time.perf_counter() - t1
+
+    run(2)
+    prompt, tokens = run(a.generate)
+    print(json.dumps(dict(model=a.model, blocks=a.blocks, requests=a.requests, prompt=a.prompt, generate=a.generate, k_format=a.k_format, v_format=a.v_format,
+                          read_blocks=a.read_blocks, prompt_ms=prompt * 1e3, token_ms=tokens * 1e3 / max(a.generate, 1), cache_mib=blocks.cache_bytes() / 2**20,
+                          cache_mib_bf16=a.requests * (a.prompt + a.generate) * 4 * shape.n_kv_heads * shape.head_dim * a.blocks / 2**20)))
+
+
+if __name__ == "__main__":
+    main()

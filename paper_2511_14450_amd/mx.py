@@ -157,25 +157,27 @@ class MxCache:
 
     @classmethod
     def allocate(cls, n_requests: int, n_kv_heads: int, most: int, head_dim: int, k_format: str = "e4m3", v_format: str = "e4m3", block_keys: int = 0,
-                 page_keys: int = 0, n_pages: Optional[int] = None, device="cuda") -> "MxCache":
+                 page_keys: int = 0, n_pages: Optional[int] = None, lens: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None,
+                 device="cuda") -> "MxCache":
         """An empty cache with memory of its own: slabs, or pages of page_keys keys (n_pages of them, by default enough for all; request b has pages
-        b * ceil(most / page_keys) on until the caller writes another table).  block_keys > 0: with bounds of such blocks.  Its tensors are the
-        attributes k, v, k_scale, v_scale, lens, page_table, lo and hi."""
+        b * ceil(most / page_keys) on until the caller writes another table).  block_keys > 0: with bounds of such blocks.  lens, page_table: where
+        several caches, of a model's blocks, share them.  Its tensors are the attributes k, v, k_scale, v_scale, lens, page_table, lo and hi."""
         for name in (k_format, v_format):
             _need(name in MX_FORMATS, f"format: need one of {', '.join(MX_FORMATS)}")
-        groups, unit = -(-head_dim // 32), max(16, block_keys)
-        table = None
+        groups, unit, table = -(-head_dim // 32), max(16, block_keys), page_table
+        _need(page_table is None or page_keys, "page_table goes with page_keys")
         if page_keys:
             per = -(-most // page_keys)
             slabs, room = n_requests * per if n_pages is None else n_pages, page_keys
-            table = torch.arange(n_requests * per, dtype=torch.int32, device=device).reshape(n_requests, per)
+            if table is None:
+                table = torch.arange(n_requests * per, dtype=torch.int32, device=device).reshape(n_requests, per)
         else:
             slabs, room = n_requests, -(-most // unit) * unit
         new = lambda *shape, dtype=torch.uint8: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
         k, v = (new(slabs, n_kv_heads, room, _GROUP_BYTES[MX_FORMATS[f]] * groups) for f in (k_format, v_format))
         k_scale, v_scale = (new(slabs, n_kv_heads, groups, room) for _ in range(2))
         lo, hi = (new(slabs, n_kv_heads, room // block_keys, head_dim, dtype=torch.bfloat16) if block_keys else None for _ in range(2))
-        return cls(k, v, k_scale, v_scale, new(n_requests, dtype=torch.int32), head_dim, page_table=table, most=most, lo=lo, hi=hi)
+        return cls(k, v, k_scale, v_scale, new(n_requests, dtype=torch.int32) if lens is None else lens, head_dim, page_table=table, most=most, lo=lo, hi=hi)
 
     k, v, k_scale, v_scale, lens, page_table, lo, hi = (property(lambda self, i=i: self._keep[i]) for i in range(8))
 
@@ -189,21 +191,20 @@ def mx_write(cache: MxCache, k: torch.Tensor, v: torch.Tensor, q_start: Optional
     """Quantises rows [rows, kv heads, d] (f32 or bf16), the newest keys of every request, into the cache: request b has rows q_start[b] ..
     q_start[b + 1] - 1 (no q_start: row b); the numbers that are stored also go to k_out and v_out, which may be k and v."""
     index, nkv, d = cache.index, cache.n_kv_heads, cache.head_dim
-    shape = k.shape
+    shape, dtype = k.shape, k.dtype
     _need((k_out is None) == (v_out is None), "k_out and v_out go together")
     for t, name in ((k, "k"), (v, "v")) if k_out is None else ((k, "k"), (v, "v"), (k_out, "k_out"), (v_out, "v_out")):
-        if t.dim() != 3 or t.shape != shape or t.dtype != k.dtype or t.get_device() != index or not _features(t, d):
+        if len(shape) != 3 or t.shape != shape or t.dtype != dtype or t.get_device() != index or (t.stride(2) != 1 and d != 1):
             raise ValueError(f"{name}: need a tensor of k's shape and type on the cache's device, features contiguous")
-    if k.dtype not in _DTYPES or shape[1] != nkv or shape[2] != d:
+    if dtype not in _DTYPES or shape[1] != nkv or shape[2] != d:
         raise ValueError(f"k: need a float32 or bfloat16 tensor [rows, {nkv}, {d}]")
-    rows = _MxRows(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
-    if k_out is not None:
-        rows.k_out, rows.v_out = k_out.data_ptr(), v_out.data_ptr()
-        rows.k_out_row_stride, rows.k_out_head_stride = k_out.stride()[:2]
-        rows.v_out_row_stride, rows.v_out_head_stride = v_out.stride()[:2]
-    rows.n_rows, rows.dtype = shape[0], _DTYPES[k.dtype]
-    if q_start is not None:
-        rows.q_start = _ints(q_start, (cache.n_requests + 1,), "q_start", index)
+    ks, vs = k.stride(), v.stride()
+    start = None if q_start is None else _ints(q_start, (cache.n_requests + 1,), "q_start", index)
+    if k_out is None:
+        rows = _MxRows(k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], None, None, 0, 0, 0, 0, shape[0], start, _DTYPES[dtype])
+    else:
+        ko, vo = k_out.stride(), v_out.stride()
+        rows = _MxRows(k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], k_out.data_ptr(), v_out.data_ptr(), ko[0], ko[1], vo[0], vo[1], shape[0], start, _DTYPES[dtype])
     with _on(stream):
         _check(_lib().mx_write(cache._ref, C.byref(rows), _handle(stream, index)))
 
@@ -222,10 +223,11 @@ def mx_read(cache: MxCache, k: torch.Tensor, v: torch.Tensor, first: Optional[to
 
 
 def _q(cache: MxCache, q: torch.Tensor) -> _MxQ:
-    if (q.dim() != 3 or q.dtype not in _DTYPES or q.get_device() != cache.index or q.shape[0] != cache.n_requests or q.shape[2] != cache.head_dim
-            or not _features(q, cache.head_dim)):
-        raise ValueError(f"q: need a float32 or bfloat16 tensor [{cache.n_requests}, query heads, {cache.head_dim}] on the cache's device, features contiguous")
-    return _MxQ(q.data_ptr(), q.stride(0), q.stride(1), _int32(q.shape[1], "query heads"), _DTYPES[q.dtype])
+    shape, stride, d = q.shape, q.stride(), cache.head_dim
+    if (len(shape) != 3 or q.dtype not in _DTYPES or q.get_device() != cache.index or shape[0] != cache.n_requests or shape[2] != d
+            or (stride[2] != 1 and d != 1)):
+        raise ValueError(f"q: need a float32 or bfloat16 tensor [{cache.n_requests}, query heads, {d}] on the cache's device, features contiguous")
+    return _MxQ(q.data_ptr(), stride[0], stride[1], _int32(shape[1], "query heads"), _DTYPES[q.dtype])
 
 
 def mx_select_workspace_bytes(cache: MxCache, q: torch.Tensor, keep: int) -> int:
@@ -259,26 +261,29 @@ def mx_token(cache: MxCache, rule: AttnRule, q: torch.Tensor, blocks: Optional[t
              lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
              stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(out, lse) of one row a request, q [n, query heads, d], its newest key: over all keys, or over those of blocks [n, kv heads, listed] (int32)."""
-    lib = _lib()
-    index = cache.index
+    lib, index = _lib(), cache.index
     with _on(stream):
-        row = C.byref(_q(cache, q))
-        _need(rule.n_q_heads is None or (rule.n_q_heads == q.shape[1] and rule.index == index), "slopes: need one for each query head, on the cache's device")
+        row, shape = C.byref(_q(cache, q)), q.shape
+        if rule.n_q_heads is not None and (rule.n_q_heads != shape[1] or rule.index != index):
+            raise ValueError("slopes: need one for each query head, on the cache's device")
         listed, ptr = 0, None
         if blocks is not None:
             _need(blocks.dim() == 3 and blocks.shape[2] >= 1, "blocks: need [requests, kv heads, blocks]")
             listed = _int32(blocks.shape[2], "blocks")
             ptr = _ints(blocks, (cache.n_requests, cache.n_kv_heads, listed), "blocks", index)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=cache.device)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.get_device() != index or not _features(out, cache.head_dim):
+            out = torch.empty_like(q)  # of a dense q with its order of strides, else contiguous
+        elif out.shape != shape or out.dtype != q.dtype or out.get_device() != index or not _features(out, cache.head_dim):
             raise ValueError("out: need a tensor of q's shape and type on its device, features contiguous")
         if lse is None:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=cache.device)
-        elif lse.shape != q.shape[:2] or lse.dtype != torch.float32 or lse.get_device() != index or not lse.is_contiguous():
+            lse = q.new_empty(shape[:2], dtype=torch.float32)
+        elif lse.shape != shape[:2] or lse.dtype != torch.float32 or lse.get_device() != index or not lse.is_contiguous():
             raise ValueError("lse: need a contiguous float32 tensor [requests, query heads] on the cache's device")
-        need = lib.mx_token_workspace_bytes(cache._ref, row, listed) if workspace is None else 0
-        workspace, work, size = _workspace(need, workspace, cache.device)
-        o = _Out(out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr())
-        _check(lib.mx_token(cache._ref, rule._ref, row, ptr, listed, C.byref(o), work, size, _handle(stream, index)))
+        work, size = None, 0
+        if workspace is not None or (size := lib.mx_token_workspace_bytes(cache._ref, row, listed)):
+            workspace, work, size = _workspace(size, workspace, cache.device)
+        stride = out.stride()
+        status = lib.mx_token(cache._ref, rule._ref, row, ptr, listed, C.byref(_Out(out.data_ptr(), stride[0], stride[1], lse.data_ptr())), work, size, _handle(stream, index))
+        if status:
+            _check(status)
     return out, lse

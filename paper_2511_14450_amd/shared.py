@@ -36,39 +36,15 @@ def shared_prefix(stage: binding.Stage, l_start: int, l_end: int, request: int =
     return out
 
 
-class SharedBlocks:
-    """Blocks over n_requests requests that share `prefix` (shared_prefix of the same blocks).
+class BlockMath:
+    """What a block computes besides its attention, in PyTorch: projections, norms, rotary positions and the FFN.  Keys are rotated before they are
+    cached."""
 
-    budget  own keys of a request and KV head that stay after its prompt and after an eviction
-    room    tokens between evictions
-    sink, recent  how many of the first and the newest own keys always stay
-    window  rows of a prompt's end whose attention decides which of its keys stay (0: all of them)
-    """
-
-    def __init__(self, shape, layers: Sequence[Dict[str, torch.Tensor]], prefix: Sequence[Tuple[torch.Tensor, torch.Tensor]],
-                 n_requests: int, budget: int, room: int, sink: int = 4, recent: int = 32, window: int = 64):
-        if len(prefix) != len(layers):
-            raise ValueError("prefix: need keys and values of every block")
-        if budget < 1 or room < 1 or sink < 0 or recent < 0 or sink + recent > budget:
-            raise ValueError("need budget and room of at least 1, and sink + recent within the budget")
-        self.shape, self.layers, self.prefix = shape, list(layers), list(prefix)
-        self.n, self.budget, self.room, self.sink, self.recent, self.window = n_requests, budget, room, sink, recent, window
-        self.prefix_len = prefix[0][0].shape[1] if prefix else 0
+    def __init__(self, shape, layers: Sequence[Dict[str, torch.Tensor]]):
+        self.shape, self.layers = shape, list(layers)
         self.rule = attn.AttnRule(shape.head_dim ** -0.5)
         i = torch.arange(shape.head_dim // 2, dtype=torch.float64, device="cuda")
         self.angle = shape.rope_base ** (-2.0 * i / shape.head_dim)
-        dtype = prefix[0][0].dtype
-        sizes = (n_requests, shape.n_kv_heads, budget + room)
-        self.k = [torch.empty((*sizes, shape.head_dim), dtype=dtype, device="cuda") for _ in layers]
-        self.v = [torch.empty_like(k) for k in self.k]
-        self.pos = [torch.zeros(sizes, dtype=torch.int32, device="cuda") for _ in layers]
-        self.totals = [torch.zeros(sizes, dtype=torch.float32, device="cuda") for _ in layers]
-        self.lens = [torch.zeros(n_requests, dtype=torch.int32, device="cuda") for _ in layers]
-        self.caches = [attn.AttnCache(k, v, n, prefix_k=p[0], prefix_v=p[1], key_pos=pos)
-                       for k, v, n, p, pos in zip(self.k, self.v, self.lens, self.prefix, self.pos)]
-        self.now = torch.full((n_requests,), self.prefix_len, dtype=torch.int32, device="cuda")  # position of the next token
-        self.most = 0  # keys that the longest request holds
-        self.requests = torch.arange(n_requests, device="cuda")
 
     def _norm(self, x, g):
         y = x.float()
@@ -92,6 +68,39 @@ class SharedBlocks:
         x = x + F.linear(out.reshape(x.shape[0], -1), w["wo"])
         h = self._norm(x, w["ffn_norm_g"])
         return x + F.linear(F.silu(F.linear(h, w["w_gate"])) * F.linear(h, w["w_up"]), w["w_down"])
+
+
+class SharedBlocks(BlockMath):
+    """Blocks over n_requests requests that share `prefix` (shared_prefix of the same blocks).
+
+    budget  own keys of a request and KV head that stay after its prompt and after an eviction
+    room    tokens between evictions
+    sink, recent  how many of the first and the newest own keys always stay
+    window  rows of a prompt's end whose attention decides which of its keys stay (0: all of them)
+    """
+
+    def __init__(self, shape, layers: Sequence[Dict[str, torch.Tensor]], prefix: Sequence[Tuple[torch.Tensor, torch.Tensor]],
+                 n_requests: int, budget: int, room: int, sink: int = 4, recent: int = 32, window: int = 64):
+        if len(prefix) != len(layers):
+            raise ValueError("prefix: need keys and values of every block")
+        if budget < 1 or room < 1 or sink < 0 or recent < 0 or sink + recent > budget:
+            raise ValueError("need budget and room of at least 1, and sink + recent within the budget")
+        super().__init__(shape, layers)
+        self.prefix = list(prefix)
+        self.n, self.budget, self.room, self.sink, self.recent, self.window = n_requests, budget, room, sink, recent, window
+        self.prefix_len = prefix[0][0].shape[1] if prefix else 0
+        dtype = prefix[0][0].dtype
+        sizes = (n_requests, shape.n_kv_heads, budget + room)
+        self.k = [torch.empty((*sizes, shape.head_dim), dtype=dtype, device="cuda") for _ in layers]
+        self.v = [torch.empty_like(k) for k in self.k]
+        self.pos = [torch.zeros(sizes, dtype=torch.int32, device="cuda") for _ in layers]
+        self.totals = [torch.zeros(sizes, dtype=torch.float32, device="cuda") for _ in layers]
+        self.lens = [torch.zeros(n_requests, dtype=torch.int32, device="cuda") for _ in layers]
+        self.caches = [attn.AttnCache(k, v, n, prefix_k=p[0], prefix_v=p[1], key_pos=pos)
+                       for k, v, n, p, pos in zip(self.k, self.v, self.lens, self.prefix, self.pos)]
+        self.now = torch.full((n_requests,), self.prefix_len, dtype=torch.int32, device="cuda")  # position of the next token
+        self.most = 0  # keys that the longest request holds
+        self.requests = torch.arange(n_requests, device="cuda")
 
     def prefill(self, hidden: torch.Tensor, seq_lens: Sequence[int]) -> torch.Tensor:
         """Hidden states [sum(seq_lens), H] of the requests' own prompts through the blocks; their caches start anew."""
