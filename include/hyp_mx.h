@@ -21,8 +21,8 @@
  * normal float and a bf16 as it stands, and rounds feature / 2^s to the nearest number, ties to the even
  * code; what is still larger (above 1.75 * 2^127 or 1.5 * 2^127) becomes the largest.  A group with an
  * infinity or a NaN gets byte 255 and reads as NaN.  The last group is filled up with zeros: a key of
- * head_dim d takes ceil(d / 32) groups of 32 or 16 bytes.  Scale bytes that mx_write does not write
- * stand for code * 2^s rounded to bf16.
+ * head_dim d takes ceil(d / 32) groups of 32 or 16 bytes.  Keys under scale bytes that mx_write does not
+ * write are read as well, but what they give is not defined.
  *
  * A row is the newest key of its request (hyp_attn.h): rows are cached and counted in lens before the
  * calls that use them; of mx_write, row i of the n_b rows of request b goes to key lens[b] - n_b + i.
@@ -34,7 +34,7 @@
  * mx_last_error().  Values on the device are not trusted: lengths are cut to 0..most, row ranges to the
  * rows there are, page numbers to the pool, and blocks that a request does not hold are not read, so that
  * wrong ones give wrong numbers but no access outside the tensors.  The calls keep no state; any number
- * of threads and streams may make them.  Calls that write a request's cache and calls that read it are
+ * of threads and streams may make them, each with a workspace of its own.  Calls that write a request's cache and calls that read it are
  * the caller's to order, as are two requests whose tables name the same page.
  */
 #ifndef HYP_MX_H

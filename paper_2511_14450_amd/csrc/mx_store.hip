@@ -94,7 +94,7 @@ __device__ __forceinline__ void write_rows(const T *in, int64_t in_stride, T *ou
       if (r >= n) break;
       float y[8];
       raw[x].get(f, d, y);
-      const unsigned scale = put8<F>(codes + (unsigned)r * (unsigned)key_stride, scales + r, within, group_stride, y);
+      const unsigned scale = put8<F>(codes + (uint64_t)(unsigned)r * (unsigned)key_stride, scales + r, within, group_stride, y);
       seen(y, scale == 255u);
       if (out) store8<T, WIDE>(out + r * out_stride, f, d, y);
     }

@@ -9,6 +9,7 @@
 // products of bf16 rows are exact; float rows and probabilities are three bf16 that add up to them.
 #pragma once
 
+#include <atomic>
 #include <type_traits>
 
 #include "attn_score.h"
@@ -554,9 +555,17 @@ template <typename T, int KF, int VF, int G> hipError_t token_of(const MxTokenCa
   constexpr int most = token_lds<G, T>(16);
   static_assert(most <= 160 * 1024, "LDS of a CU");
   const int lds = token_lds<G, T>(p.G < 16 ? p.G : 16);
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void *)k_mx_token<T, G, KF, VF>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+  if (lds > 64 * 1024) {  // sixteen heads of more than 224 features: each device is told once
+    static std::atomic<uint64_t> told{0};
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute((const void *)k_mx_token<T, G, KF, VF>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+      if (e != hipSuccess) return e;
+      told.fetch_or(bit, std::memory_order_relaxed);
+    }
   }
   k_mx_token<T, G, KF, VF><<<(unsigned)p.m.c.n_requests * p.m.c.n_kv_heads * p.head_tiles * p.parts, kThreads, lds, s>>>(p);
   return hipGetLastError();

@@ -120,3 +120,17 @@ def test_two_graphs_that_share_a_workspace():
             graphs[i].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1]) for i in range(2) if turn % 3 < 2 or i == 0)
+
+
+def test_the_widest_heads_are_recorded_without_a_call_before():
+    # sixteen heads of 256 features join in more LDS than a launch has by itself
+    pr = Problem(13, [100], nkv=1, d=256, formats=("e2m1", "e4m3"), dtype=F32).fill()
+    q, out, lse = torch.randn((1, 16, 256), generator=pr.gen).cuda(), torch.zeros((1, 16, 256), device="cuda"), torch.zeros((1, 16), device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hyp.mx_token(pr.cache, hyp.AttnRule(0.0625), q, out=out, lse=lse)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = hyp.mx_token(pr.cache, hyp.AttnRule(0.0625), q)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])

@@ -204,3 +204,35 @@ def test_offsets_beyond_32_bits():
     o, z, o_abs, delta = ref.attend(q[-1, 0].cpu(), keys, keys, list(range(64)), scale=0.125)
     assert bool(((got[-1, 0].double().cpu() - o).abs() <= ref.out_bound(o, o_abs, delta, F32)).all()) and abs(float(lse[-1, 0]) - z) <= delta
     assert bool((got[:-1] == 0).all()) and bool((lse[:-1] == -math.inf).all())
+
+
+@pytest.mark.parametrize("n", [511, 512, 513, 1100])
+def test_many_requests(n):
+    # starts and lengths of up to 512 requests are read at once, of more request by request
+    held = [(i * 7) % 5 for i in range(n)]
+    pr = Problem(11, held, nkv=1, d=32, formats=("e4m3", "e4m3"), block=16, layout="pages", page=16).fill()
+    room = torch.zeros((n, 1, 4, 32), device="cuda")
+    out = [room, torch.zeros_like(room)]
+    hyp.mx_read(pr.cache, *out)
+    want = torch.cat(pr.values()[0])[:, 0]
+    got = torch.cat([out[0][b, 0, :h] for b, h in enumerate(held)])
+    assert torch.equal(got.double().cpu(), want)
+
+
+def test_keys_far_apart():
+    # a key stride just below what is allowed, in a block of 512 keys: bytes beyond 32 bits from the block's first key
+    stride, keys, d, room = (1 << 24) - 16, 300, 32, 512
+    k = torch.empty(stride * room, dtype=torch.uint8, device="cuda").view(1, 1, room, stride)[..., :32]
+    small = lambda: torch.zeros((1, 1, room, 32), dtype=torch.uint8, device="cuda")  # noqa: E731
+    scale = lambda: torch.zeros((1, 1, 1, room), dtype=torch.uint8, device="cuda")  # noqa: E731
+    lens = torch.tensor([keys], dtype=torch.int32, device="cuda")
+    lo, hi = (torch.zeros((1, 1, 1, d), dtype=BF, device="cuda") for _ in range(2))
+    cache = hyp.MxCache(k, small(), scale(), scale(), lens, d, most=keys, lo=lo, hi=hi)
+    x = torch.randn((keys, 1, d), generator=torch.Generator().manual_seed(12))
+    start = torch.tensor([0, keys], dtype=torch.int32, device="cuda")
+    hyp.mx_write(cache, x.cuda(), x.cuda(), q_start=start)
+    out = [torch.zeros((1, 1, keys, d), device="cuda") for _ in range(2)]
+    hyp.mx_read(cache, *out)
+    want = ref.stored_rows("e4m3", x[:, 0])
+    assert torch.equal(out[0][0, 0].double().cpu(), want) and torch.equal(out[1][0, 0].double().cpu(), want)
+    assert torch.equal(lo[0, 0, 0].double().cpu(), want.amin(0))
