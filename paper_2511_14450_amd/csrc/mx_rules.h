@@ -16,7 +16,10 @@ inline int64_t mx_write_tiles(int64_t rows, int64_t requests, int64_t block, boo
 // mx_select: in one launch up to so many blocks of a request, or where all are kept.
 constexpr int kMxSmallBlocks = 256;
 inline bool mx_select_once(int blocks, int keep) { return blocks <= kMxSmallBlocks || blocks <= keep; }
-// Else scores are formed by workgroups of 64 blocks once to four times: a row is converted once for all of them, but there have to be two workgroups
+// Up to so many blocks are chosen among by 512 threads, which hold them in registers, more by 1024 (64 caches of up to 2048: 23.5 us, 25.3 with 1024;
+// 16 of 7813: 35, 38 with 512).
+constexpr int kMxChooseBlocks = 2048;
+// Scores are formed by workgroups of 64 blocks once to four times: a row is converted once for all of them, but there have to be two workgroups
 // a CU.
 inline int mx_score_turns(int64_t pairs, int64_t blocks) {
   int turns = 4;

@@ -6,7 +6,7 @@ namespace hyp {
 namespace {
 
 constexpr int kThreads = 256, kHeads = 4;  // query heads whose scores are formed at a time
-constexpr int kSelectThreads = 1024, kItems = 4, kMostCandidates = kSelectThreads / 8;
+constexpr int kItems = 4;  // blocks of a thread that chooses
 
 typedef unsigned long long u64;
 
@@ -180,24 +180,25 @@ template <int WAVES> __device__ __forceinline__ int before_me(int v, int *scratc
   return before;
 }
 
-// One request and KV head with more blocks than are kept.  Scores are sorted into 2048 bins between the least and the largest; the bin in which
-// the last one falls that is taken is cut into 2048 again until it holds few, which are then ranked one by one.
-__global__ void __launch_bounds__(kSelectThreads) k_mx_choose(const MxSelectCall p) {
-  constexpr int WAVES = kSelectThreads / 64;
-  __shared__ int hist[2048], scratch[WAVES], found[3];
+// One request and KV head with more blocks than are kept.  Scores are sorted into kBins bins between the least and the largest; the bin in which
+// the last one falls that is taken is cut into as many again until it holds few, which are then ranked one by one.
+template <int THREADS> __global__ void __launch_bounds__(THREADS) k_mx_choose(const MxSelectCall p) {
+  constexpr int WAVES = THREADS / 64, kMostCandidates = THREADS / 8;
+  constexpr int kBins = 2 * THREADS, kBits = 31 - __builtin_clz(kBins);  // two bins a thread
+  __shared__ int hist[kBins], scratch[WAVES], found[3];
   __shared__ u64 ends[2], cand[kMostCandidates];
   __shared__ int cand_at[kMostCandidates];
   const int pair = blockIdx.x, b = pair / p.m.c.n_kv_heads, tid = threadIdx.x, lane = tid & 63, K = p.keep;
   const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
   int *out = p.blocks + (int64_t)pair * K;
   if (count <= K) {
-    for (int r = tid; r < K; r += kSelectThreads) out[r] = r < count ? r : -1;
+    for (int r = tid; r < K; r += THREADS) out[r] = r < count ? r : -1;
     return;
   }
   const u64 *order = p.order + (int64_t)pair * p.most_blocks;
   const int newest = count - p.recent;
   // a thread has runs of kItems blocks, so that counts in the order of threads are counts in the order of blocks
-  constexpr int STEP = kSelectThreads * kItems;
+  constexpr int STEP = THREADS * kItems;
   const bool once = count <= STEP;
   u64 u[kItems];
   auto read = [&](int base) {
@@ -243,14 +244,14 @@ __global__ void __launch_bounds__(kSelectThreads) k_mx_choose(const MxSelectCall
   // taken: all above `to`, and `need` of [from, to]
   int inside = count - always;
   while (need > 0 && need < inside && inside > kMostCandidates && from < to) {
-    const int shift = max(0, 64 - __clzll((long long)(to - from)) - 11);
-    for (int x = tid; x < 2048; x += kSelectThreads) hist[x] = 0;
+    const int shift = max(0, 64 - __clzll((long long)(to - from)) - kBits);
+    hist[tid] = hist[tid + THREADS] = 0;
     __syncthreads();
     each([&](int, u64 v) {
       if (v >= from && v <= to) atomicAdd(&hist[(int)((v - from) >> shift)], 1);
     });
     __syncthreads();
-    const int hi = 2047 - 2 * tid, own0 = hist[hi], own1 = hist[hi - 1];
+    const int hi = kBins - 1 - 2 * tid, own0 = hist[hi], own1 = hist[hi - 1];
     int all;
     const int above = before_me<WAVES>(own0 + own1, scratch, all);
     if (above < need && need <= above + own0) {
@@ -374,7 +375,8 @@ template <typename T, int N, bool WIDE> hipError_t select(const MxSelectCall &p,
   k_mx_scores<T, N, WIDE><<<pairs * tiles, kThreads, 0, s>>>(p, tiles, turns);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;  // the choice goes by the scores
-  k_mx_choose<<<pairs, kSelectThreads, 0, s>>>(p);
+  if (p.most_blocks <= kMxChooseBlocks) k_mx_choose<512><<<pairs, 512, 0, s>>>(p);
+  else k_mx_choose<1024><<<pairs, 1024, 0, s>>>(p);
   return hipGetLastError();
 }
 
