@@ -45,21 +45,19 @@ template <int F> __device__ __forceinline__ unsigned mx_scale_byte(unsigned bits
   return (unsigned)mx_clamped((int)(bits >> 23) - top + ((int)(bits & 0x7fffffu) > fraction), lo, hi);
 }
 
-// Eight features to codes (one or two words), and the numbers that are stored in their place.  Where a group is not finite the codes are NaN
-// (HYP_E4M3) or 0, and every number NaN.
-template <int F> __device__ __forceinline__ void mx_quantise(float (&x)[8], unsigned scale, unsigned (&w)[2]) {
+// Eight features to codes (one or two words), and the numbers that are stored in their place, as pairs of bf16.  Where a group is not finite the codes
+// are NaN (HYP_E4M3) or 0, and every number NaN.
+template <int F> __device__ __forceinline__ void mx_quantise(const float (&x)[8], unsigned scale, unsigned (&w)[2], unsigned (&pairs)[4]) {
   constexpr float most = F == HYP_E4M3 ? 448.f : 6.f;
-  const bool bad = scale == 255u;
   const float down = __uint_as_float((254u - scale) << 23), up = mx_scale(scale);  // scale lies in 2..252
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = bad ? 0.f : fminf(fmaxf(x[i] * down, -most), most);
+  for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i] * down, -most, most);
   if constexpr (F == HYP_E4M3) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h], y[4 * h + 1], 0, false);
-      c = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], c, true);
-      w[h] = bad ? 0x7f7f7f7fu : (unsigned)c;
+      w[h] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], c, true);
     }
   } else {
     unsigned c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], 1.0f, 0);
@@ -69,10 +67,13 @@ template <int F> __device__ __forceinline__ void mx_quantise(float (&x)[8], unsi
     w[1] = 0;
   }
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const unsigned r = mx_pair<F>(w, p, up);
-    x[2 * p] = __uint_as_float(r << 16);
-    x[2 * p + 1] = __uint_as_float(r & 0xffff0000u);
+  for (int p = 0; p < 4; ++p) pairs[p] = mx_pair<F>(w, p, up);
+  const bool bad = scale == 255u;
+  if (__any(bad)) {
+    w[0] = bad ? (F == HYP_E4M3 ? 0x7f7f7f7fu : 0u) : w[0];
+    w[1] = bad ? (F == HYP_E4M3 ? 0x7f7f7f7fu : 0u) : w[1];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) pairs[p] = bad ? 0x7fc07fc0u : pairs[p];
   }
 }
 

@@ -35,22 +35,23 @@ template <typename T, bool WIDE> struct Eight {
 
 // Rows are read and written once here and are larger than what the caches hold: streaming loads and stores leave those to the codes (reading
 // four caches of 6007 to 8192 keys back 41 us without, 30 with; 4 x 8192 rows into 4 bits 72 and 62).
-template <typename T, bool WIDE> __device__ __forceinline__ void store8(T *row, int f, int d, const float (&x)[8]) {
+__device__ __forceinline__ float low_of(unsigned pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float high_of(unsigned pair) { return __uint_as_float(pair & 0xffff0000u); }
+template <typename T, bool WIDE> __device__ __forceinline__ void store8(T *row, int f, int d, const unsigned (&pairs)[4]) {
   if constexpr (WIDE) {
     if (f >= d) return;
     if constexpr (sizeof(T) == 2) {
-      u16x8_t v;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v.v[i] = f32_to_bf16(x[i]);
+      const uint4 v = make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]);
       __builtin_nontemporal_store(__builtin_bit_cast(f32x4_t, v), (f32x4_t *)(row + f));
     } else {
-      __builtin_nontemporal_store(f32x4_t{x[0], x[1], x[2], x[3]}, (f32x4_t *)(row + f));
-      __builtin_nontemporal_store(f32x4_t{x[4], x[5], x[6], x[7]}, (f32x4_t *)(row + f + 4));
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        __builtin_nontemporal_store(f32x4_t{low_of(pairs[2 * i]), high_of(pairs[2 * i]), low_of(pairs[2 * i + 1]), high_of(pairs[2 * i + 1])}, (f32x4_t *)(row + f + 4 * i));
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (f + i < d) store_f32(row + f + i, x[i]);
+      if (f + i < d) store_f32(row + f + i, i & 1 ? high_of(pairs[i >> 1]) : low_of(pairs[i >> 1]));
   }
 }
 
@@ -63,11 +64,11 @@ __device__ __forceinline__ unsigned group_most(const float (&x)[8]) {
   return max(m, quad_xor<2>(m));
 }
 
-// Codes and scale of eight features; x becomes the numbers that are stored.
-template <int F> __device__ __forceinline__ unsigned put8(uint8_t *codes, uint8_t *scales, int within, int64_t group_stride, float (&x)[8]) {
+// Codes and scale of eight features, and the numbers that are stored.
+template <int F> __device__ __forceinline__ unsigned put8(uint8_t *codes, uint8_t *scales, int within, int64_t group_stride, const float (&x)[8], unsigned (&pairs)[4]) {
   const unsigned scale = mx_scale_byte<F>(group_most(x));
   unsigned w[2];
-  mx_quantise<F>(x, scale, w);
+  mx_quantise<F>(x, scale, w, pairs);
   if constexpr (F == HYP_E4M3) *(uint2 *)(codes + 8 * within) = make_uint2(w[0], w[1]);
   else *(unsigned *)(codes + 4 * within) = w[0];
   if ((within & 3) == 0) scales[(within >> 2) * group_stride] = (uint8_t)scale;
@@ -93,10 +94,11 @@ __device__ __forceinline__ void write_rows(const T *in, int64_t in_stride, T *ou
       const int r = base + x * step;
       if (r >= n) break;
       float y[8];
+      unsigned pairs[4];
       raw[x].get(f, d, y);
-      const unsigned scale = put8<F>(codes + (uint64_t)(unsigned)r * (unsigned)key_stride, scales + r, within, group_stride, y);
-      seen(y, scale == 255u);
-      if (out) store8<T, WIDE>(out + r * out_stride, f, d, y);
+      const unsigned scale = put8<F>(codes + (uint64_t)(unsigned)r * (unsigned)key_stride, scales + r, within, group_stride, y, pairs);
+      seen(pairs, scale == 255u);
+      if (out) store8<T, WIDE>(out + r * out_stride, f, d, pairs);
     }
   }
 }
@@ -163,18 +165,20 @@ template <typename T, bool WIDE, int KF, int VF> __global__ void __launch_bounds
                               p.r.v_out ? (T *)p.r.v_out + row0 * p.r.v_out_row_stride + head * p.r.v_out_head_stride : nullptr, p.r.v_out_row_stride,
                               c.v + page * c.v_page_stride + head * c.v_head_stride + at0 * c.v_key_stride, c.v_key_stride,
                               c.v_scale + page * c.v_scale_page_stride + head * c.v_scale_head_stride + at0, c.v_scale_group_stride, within, mine, step, j1 - j0, d,
-                              [](const float (&)[8], bool) {});
+                              [](const unsigned (&)[4], bool) {});
     } else {
       write_rows<T, KF, WIDE>((const T *)p.r.k + row0 * p.r.k_row_stride + head * p.r.k_head_stride, p.r.k_row_stride,
                               p.r.k_out ? (T *)p.r.k_out + row0 * p.r.k_out_row_stride + head * p.r.k_out_head_stride : nullptr, p.r.k_out_row_stride,
                               c.k + page * c.k_page_stride + head * c.k_head_stride + at0 * c.k_key_stride, c.k_key_stride,
                               c.k_scale + page * c.k_scale_page_stride + head * c.k_scale_head_stride + at0, c.k_scale_group_stride, within, mine, step, j1 - j0, d,
-                              [&](const float (&x)[8], bool nan) {
+                              [&](const unsigned (&pairs)[4], bool nan) {
+                                if (!bounds) return;
                                 bad |= nan;
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) {
-                                  lo[i] = fminf(lo[i], x[i]);
-                                  hi[i] = fmaxf(hi[i], x[i]);
+                                  const float x = i & 1 ? high_of(pairs[i >> 1]) : low_of(pairs[i >> 1]);
+                                  lo[i] = fminf(lo[i], x);
+                                  hi[i] = fmaxf(hi[i], x);
                                 }
                               });
     }
@@ -214,14 +218,10 @@ constexpr int kReadKeys = 64;
 template <typename T, int F, bool WIDE> __device__ __forceinline__ void get8(uint2 codes, unsigned scale_byte, int within, T *to, int d) {
   const unsigned w[2] = {codes.x, codes.y};
   const float scale = mx_scale(scale_byte);
-  float x[8];
+  unsigned pairs[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned r = mx_pair<F>(w, i, scale);
-    x[2 * i] = __uint_as_float(r << 16);
-    x[2 * i + 1] = __uint_as_float(r & 0xffff0000u);
-  }
-  store8<T, WIDE>(to, 8 * within, d, x);
+  for (int i = 0; i < 4; ++i) pairs[i] = mx_pair<F>(w, i, scale);
+  store8<T, WIDE>(to, 8 * within, d, pairs);
 }
 
 template <typename T, bool WIDE, int KF, int VF> __global__ void __launch_bounds__(kThreads) k_mx_read(const MxReadCall p) {
