@@ -88,7 +88,7 @@ void check_listed(const hyp_mx_cache_t &c, int32_t listed) {
 // The cut of a call, and its workspace: floats of partial sums, of (maximum, sum) pairs.
 struct Plan {
   MxTokenPlan cut;
-  int group, head_tiles;
+  int group;
   int64_t items, part_o = 0, part_ml = 0;
   size_t bytes() const { return (size_t)(part_o + part_ml) * 4; }
 };
@@ -96,10 +96,9 @@ Plan plan_token(const MxCache &m, const hyp_mx_q_t &q, int32_t listed) {
   const hyp_mx_cache_t &c = m.c;
   Plan p = {};
   p.group = q.n_q_heads / c.n_kv_heads;
-  p.head_tiles = (p.group + 15) / 16;
-  p.items = (int64_t)c.n_requests * c.n_kv_heads * p.head_tiles;
-  p.cut = mx_token_plan(p.items, listed ? (int64_t)listed << m.block_shift : c.most, c.page_keys, listed ? c.block_keys : 0,
-                        m.groups * ((c.k_format == HYP_E4M3 ? 32 : 16) + (c.v_format == HYP_E4M3 ? 32 : 16) + 2), q.dtype == HYP_F32);
+  p.cut = mx_token_plan((int64_t)c.n_requests * c.n_kv_heads, p.group, listed ? (int64_t)listed << m.block_shift : c.most, c.page_keys, listed ? c.block_keys : 0,
+                        m.groups * ((c.k_format == HYP_E4M3 ? 32 : 16) + (c.v_format == HYP_E4M3 ? 32 : 16) + 2), m.groups, q.dtype == HYP_F32);
+  p.items = (int64_t)c.n_requests * c.n_kv_heads * p.cut.head_tiles;
   check_launch(p.items * p.cut.parts, 256);
   if (p.cut.parts > 1) {
     const int64_t rows = (int64_t)c.n_requests * q.n_q_heads;
@@ -269,7 +268,8 @@ hyp_status_t mx_token(const hyp_mx_cache_t *cache, const hyp_attn_rule_t *rule, 
     p.out_hs = out->out_head_stride;
     p.lse = out->lse;
     p.G = w.group;
-    p.head_tiles = w.head_tiles;
+    p.tiles = w.cut.tiles;
+    p.head_tiles = w.cut.head_tiles;
     p.unit = w.cut.unit;
     p.units = w.cut.units;
     p.parts = w.cut.parts;

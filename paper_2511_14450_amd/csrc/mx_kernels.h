@@ -48,7 +48,7 @@ struct MxTokenCall {
   void *out;
   int64_t out_rs, out_hs;
   float *lse;
-  int G, head_tiles;          // query heads of a KV head, tiles of 16 of them
+  int G, tiles, head_tiles;   // query heads of a KV head, tiles of 16 of them of a wave, workgroups that share them
   int unit, units, parts;     // log2(keys of a unit), units of a part
   float *part_o, *part_ml;    // [part][row][d] sums, and (maximum, sum)
   int wide_q;                 // eight features of a row at once

@@ -96,7 +96,8 @@ template <int PARTS> __device__ __forceinline__ void split8(const float (&x)[8],
   }
 }
 
-template <typename T, int G, int KF, int VF> struct Token {
+// HT: tiles of 16 query heads of a wave
+template <typename T, int G, int KF, int VF, int HT> struct Token {
   static constexpr int QP = sizeof(T) == 4 ? 3 : 1;  // parts of rows and probabilities
   static constexpr Pieces<G, KF, true> KP{};
   static constexpr Pieces<G, VF, false> VP{};
@@ -115,9 +116,9 @@ template <typename T, int G, int KF, int VF> struct Token {
   const int lane, col, quarter;
   // bytes from a run's first key to this lane's keys and values, and to their scales (key strides are below 2^24, group strides below 2^28)
   unsigned k_at, v_at[4], ks_at[KP.n], vs_at[VP.n];
-  bf16x8_t q[QP][G];
-  f32x4_t o[2 * G];
-  float m, l;
+  bf16x8_t q[HT][QP][G];
+  f32x4_t o[HT][2 * G];
+  float m[HT], l[HT];
 
   __device__ __forceinline__ Token(const MxTokenCall &call) : p(call), lane(threadIdx.x & 63), col(lane & 15), quarter(lane >> 4) {}
 
@@ -138,8 +139,8 @@ template <typename T, int G, int KF, int VF> struct Token {
     return S.base[s] + S.feats[s] * quarter;
   }
 
-  // Row of head `head` (of q), as the N operand of the steps of K's pieces; zeros where there is no such head
-  __device__ __forceinline__ void load_q(int b, int head, bool there) {
+  // Row of head `head` (of q), as tile ht's N operand of the steps of K's pieces; zeros where there is no such head
+  __device__ __forceinline__ void load_q(int ht, int b, int head, bool there) {
     const T *row = (const T *)p.q.q + b * p.q.q_row_stride + head * p.q.q_head_stride;
     const int d = p.m.c.head_dim;
     constexpr int W = 2 * sizeof(T);     // words of eight features
@@ -176,7 +177,7 @@ template <typename T, int G, int KF, int VF> struct Token {
 #pragma unroll
     for (int s = 0; s < G; ++s) {
       if constexpr (QP == 1) {
-        q[0][s] = as_bf16x8(x[s]);
+        q[ht][0][s] = as_bf16x8(x[s]);
       } else {
         float y[8];
 #pragma unroll
@@ -184,16 +185,19 @@ template <typename T, int G, int KF, int VF> struct Token {
         bf16x8_t part[QP];
         split8<QP>(y, part);
 #pragma unroll
-        for (int t = 0; t < QP; ++t) q[t][s] = part[t];
+        for (int t = 0; t < QP; ++t) q[ht][t][s] = part[t];
       }
     }
   }
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < 2 * G; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    m = kLowest;
-    l = 0.f;
+    for (int h = 0; h < HT; ++h) {
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i) o[h][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      m[h] = kLowest;
+      l[h] = 0.f;
+    }
   }
 
   __device__ __forceinline__ void aim() {
@@ -246,9 +250,10 @@ template <typename T, int G, int KF, int VF> struct Token {
     for (int i = 0; i < VP.n; ++i) r.vs[i] = *(const unsigned *)(vs + vs_at[i]);
   }
 
-  // Raw scores of a run: keys 4 quarter + i of it with this lane's head
-  __device__ __forceinline__ f32x4_t scores(const Run &r) {
-    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  // Raw scores of a run: keys 4 quarter + i of it with this lane's heads
+  __device__ __forceinline__ void scores(const Run &r, f32x4_t (&s)[HT]) {
+#pragma unroll
+    for (int h = 0; h < HT; ++h) s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     int step = 0, w = 0;
 #pragma unroll
     for (int i = 0; i < KP.n; ++i) {
@@ -262,10 +267,11 @@ template <typename T, int G, int KF, int VF> struct Token {
         w += KF == HYP_E4M3 ? 2 : 1;
         const bf16x8_t key = as_bf16x8(a);
 #pragma unroll
-        for (int t = 0; t < QP; ++t) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[t][step], s, 0, 0, 0);
+        for (int h = 0; h < HT; ++h)
+#pragma unroll
+          for (int t = 0; t < QP; ++t) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[h][t][step], s[h], 0, 0, 0);
       }
     }
-    return s;
   }
 
   // Scores of keys first + 4 quarter + i as exponents of two, -infinity where there is no such key; raw: all lie where the polynomial of a cap holds
@@ -298,35 +304,41 @@ template <typename T, int G, int KF, int VF> struct Token {
     }
   }
 
-  __device__ __forceinline__ void step(Run &a, Run &b, float slope2, int len) {
-    f32x4_t s0 = scores(a), s1 = scores(b);
-    bool raw = false;
-    if (p.cap2 != 0.f) {
-      const float far = fmaxf(fmaxf(fmaxf(fabsf(s0[0]), fabsf(s0[1])), fmaxf(fabsf(s0[2]), fabsf(s0[3]))), fmaxf(fmaxf(fabsf(s1[0]), fabsf(s1[1])), fmaxf(fabsf(s1[2]), fabsf(s1[3]))));
-      raw = !__any(!(far <= p.cap_most));  // a NaN stays one by either way
-    }
-    shape(s0, a, slope2, len, raw);
-    shape(s1, b, slope2, len, raw);
-    float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-    if (__any(top > m + kFollow)) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float now = fmaxf(m, top), f = exp2_(m - now);
+  __device__ __forceinline__ void step(Run &a, Run &b, const float (&slope2)[HT], int len) {
+    f32x4_t s0[HT], s1[HT];
+    scores(a, s0);
+    scores(b, s1);
+    bf16x8_t prob[HT][QP];
 #pragma unroll
-      for (int i = 0; i < 2 * G; ++i) o[i] *= f;
-      l *= f;
-      m = now;
-    }
-    float x[8];
+    for (int h = 0; h < HT; ++h) {
+      bool raw = false;
+      if (p.cap2 != 0.f) {
+        const float far = fmaxf(fmaxf(fmaxf(fabsf(s0[h][0]), fabsf(s0[h][1])), fmaxf(fabsf(s0[h][2]), fabsf(s0[h][3]))),
+                                fmaxf(fmaxf(fabsf(s1[h][0]), fabsf(s1[h][1])), fmaxf(fabsf(s1[h][2]), fabsf(s1[h][3]))));
+        raw = !__any(!(far <= p.cap_most));  // a NaN stays one by either way
+      }
+      shape(s0[h], a, slope2[h], len, raw);
+      shape(s1[h], b, slope2[h], len, raw);
+      float top = fmaxf(fmaxf(fmaxf(s0[h][0], s0[h][1]), fmaxf(s0[h][2], s0[h][3])), fmaxf(fmaxf(s1[h][0], s1[h][1]), fmaxf(s1[h][2], s1[h][3])));
+      if (__any(top > m[h] + kFollow)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m[h], top), f = exp2_(m[h] - now);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = exp2_(s0[i] - m);
-      x[4 + i] = exp2_(s1[i] - m);
-    }
+        for (int i = 0; i < 2 * G; ++i) o[h][i] *= f;
+        l[h] *= f;
+        m[h] = now;
+      }
+      float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) l += x[i];
-    bf16x8_t prob[QP];
-    split8<QP>(x, prob);
+      for (int i = 0; i < 4; ++i) {
+        x[i] = exp2_(s0[h][i] - m[h]);
+        x[4 + i] = exp2_(s1[h][i] - m[h]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) l[h] += x[i];
+      split8<QP>(x, prob[h]);
+    }
     if (a.valid < 16) mend(a);
     if (b.valid < 16) mend(b);
     int w = 0, at = 0;
@@ -353,10 +365,12 @@ template <typename T, int G, int KF, int VF> struct Token {
           odd[j] = __builtin_amdgcn_perm(pair[2 * j + 1], pair[2 * j], 0x07060302u);
         }
 #pragma unroll
-        for (int x = 0; x < QP; ++x) {
-          o[at] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), prob[x], o[at], 0, 0, 0);
-          o[at + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), prob[x], o[at + 1], 0, 0, 0);
-        }
+        for (int h = 0; h < HT; ++h)
+#pragma unroll
+          for (int x = 0; x < QP; ++x) {
+            o[h][at] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), prob[h][x], o[h][at], 0, 0, 0);
+            o[h][at + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), prob[h][x], o[h][at + 1], 0, 0, 0);
+          }
         at += 2;
       }
       w += words(piece_bytes(VF, P.at[i].feats));
@@ -388,10 +402,10 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// One part of a request's keys, of one KV head and up to 16 of its query heads: the waves take pairs of runs in turn, and join what they have in
+// One part of a request's keys, of one KV head and up to 16 HT of its query heads: the waves take pairs of runs in turn, and join what they have in
 // LDS.
-template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && G > 6 ? 1 : 2) k_mx_token(const MxTokenCall p) {
-  using Tk = Token<T, G, KF, VF>;
+template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && G > 6 ? 1 : 2) k_mx_token(const MxTokenCall p) {
+  using Tk = Token<T, G, KF, VF, HT>;
   extern __shared__ char lds[];
   Place *places = (Place *)lds;
   const hyp_mx_cache_t &c = p.m.c;
@@ -401,10 +415,14 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
   const int unit = 1 << p.unit, u0 = part * p.units;
   const int len = mx_len(c, b), most = p.listed ? p.listed << per : (int)(((int64_t)c.most + unit - 1) >> p.unit);
   Tk t(p);
-  const int head = ht * 16 + t.col;      // of the group
-  const bool there = head < p.G;
-  const int qh = kvh * p.G + (there ? head : 0);
-  t.load_q(b, qh, there);
+  const int head0 = ht * 16 * HT;        // of the group
+  float slope2[HT];
+#pragma unroll
+  for (int h = 0; h < HT; ++h) {
+    const int head = head0 + 16 * h + t.col, qh = kvh * p.G + (head < p.G ? head : 0);
+    t.load_q(h, b, qh, head < p.G);
+    slope2[h] = p.slopes && head < p.G ? p.slopes[qh] * kLog2e : 0.f;
+  }
   // all units that the part can have, so that nothing waits for the length; those behind the last one that holds keys are left out below
   for (int i = threadIdx.x; i < min(p.units, most - u0); i += kThreads) {
     const int u = u0 + i;
@@ -436,7 +454,6 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
   __syncthreads();
   t.aim();
   t.clear();
-  const float slope2 = p.slopes && there ? p.slopes[qh] * kLog2e : 0.f;
   auto fetch = [&](typename Tk::Run &a, typename Tk::Run &z, int i) {
     const Place at = places[i];
     const int first = __builtin_amdgcn_readfirstlane(at.first), valid = p.listed ? __builtin_amdgcn_readfirstlane(at.valid) : len - first;
@@ -454,7 +471,7 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
   };
   const int each = p.unit == 5 ? 1 : 2, STEP = kWaves * each;
   int i = wave * each;
-  if constexpr (G <= (sizeof(T) == 4 ? 3 : 4)) {
+  if constexpr (HT == 1 && G <= (sizeof(T) == 4 ? 3 : 4)) {
     // the next pair of runs is on its way while one is worked on
     typename Tk::Run a[2], z[2];
     if (i < end) {
@@ -483,30 +500,35 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
     }
   }
   // join the waves: O^T is features x heads, lane (head, quarter) has features base + (4 quarter + r) feats + x
-  t.l += __shfl_xor(t.l, 16);
-  t.l += __shfl_xor(t.l, 32);
   __syncthreads();                       // places are done with
   constexpr int PITCH = Tk::D + 4;       // floats of a head; four more keep the sixteen heads off one another's banks
-  float *ml = (float *)lds, *os = ml + 2 * kWaves * 16;
-  const int heads = min(16, p.G - ht * 16);
-  if (t.quarter == 0) {
-    ml[(wave * 16 + t.col) * 2] = t.m;
-    ml[(wave * 16 + t.col) * 2 + 1] = t.l;
-  }
-  if (there) {
-    float *to = os + (wave * heads + t.col) * PITCH;
-    int at = 0;
+  constexpr int HEADS = 16 * HT;
+  float *ml = (float *)lds, *os = ml + 2 * kWaves * HEADS;
+  const int heads = min(HEADS, p.G - head0);
 #pragma unroll
-    for (int i = 0; i < Tk::VP.n; ++i) {
-      constexpr auto P = Tk::VP;
+  for (int h = 0; h < HT; ++h) {
+    t.l[h] += __shfl_xor(t.l[h], 16);
+    t.l[h] += __shfl_xor(t.l[h], 32);
+    const int mine = 16 * h + t.col;
+    if (t.quarter == 0) {
+      ml[(wave * HEADS + mine) * 2] = t.m[h];
+      ml[(wave * HEADS + mine) * 2 + 1] = t.l[h];
+    }
+    if (mine < heads) {
+      float *to = os + (wave * heads + mine) * PITCH;
+      int at = 0;
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int i = 0; i < Tk::VP.n; ++i) {
+        constexpr auto P = Tk::VP;
 #pragma unroll
-        for (int x = 0; x < P.at[i].feats; x += 2) {
-          float2 v = make_float2(t.o[at + x][r], t.o[at + x + 1][r]);
-          *(float2 *)(to + P.at[i].base + (4 * t.quarter + r) * P.at[i].feats + x) = v;
-        }
-      at += P.at[i].feats;
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int x = 0; x < P.at[i].feats; x += 2) {
+            float2 v = make_float2(t.o[h][at + x][r], t.o[h][at + x + 1][r]);
+            *(float2 *)(to + P.at[i].base + (4 * t.quarter + r) * P.at[i].feats + x) = v;
+          }
+        at += P.at[i].feats;
+      }
     }
   }
   __syncthreads();
@@ -516,17 +538,17 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
     if (f >= d) continue;
     float top = kLowest;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[(w * 16 + h) * 2]);
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[(w * HEADS + h) * 2]);
     float sum = 0.f, s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float e = exp2_(ml[(w * 16 + h) * 2] - top);
+      const float e = exp2_(ml[(w * HEADS + h) * 2] - top);
       const float2 v = *(const float2 *)(os + (w * heads + h) * PITCH + f);
-      sum = fmaf(e, ml[(w * 16 + h) * 2 + 1], sum);
+      sum = fmaf(e, ml[(w * HEADS + h) * 2 + 1], sum);
       s0 = fmaf(e, v.x, s0);
       s1 = fmaf(e, v.y, s1);
     }
-    const int g = kvh * p.G + ht * 16 + h;
+    const int g = kvh * p.G + head0 + h;
     const int64_t row = (int64_t)b * p.q.n_q_heads + g;
     if (p.parts > 1) {
       const int64_t at = (int64_t)part * c.n_requests * p.q.n_q_heads + row;
@@ -546,43 +568,49 @@ template <typename T, int G, int KF, int VF> __global__ void __launch_bounds__(k
   }
 }
 
-template <int G, typename T> constexpr int token_lds(int heads) {
-  const int joined = 2 * kWaves * 16 * 4 + kWaves * heads * (32 * G + 4) * 4, places = kMxMostUnits * (int)sizeof(Place);
+template <int G, int HT> constexpr int token_lds(int heads) {
+  const int joined = 2 * kWaves * 16 * HT * 4 + kWaves * heads * (32 * G + 4) * 4, places = kMxMostUnits * (int)sizeof(Place);
   return joined > places ? joined : places;
 }
 
-template <typename T, int KF, int VF, int G> hipError_t token_of(const MxTokenCall &p, hipStream_t s) {
-  constexpr int most = token_lds<G, T>(16);
-  static_assert(most <= 160 * 1024, "LDS of a CU");
-  const int lds = token_lds<G, T>(p.G < 16 ? p.G : 16);
-  if (lds > 64 * 1024) {  // sixteen heads of more than 224 features: each device is told once
+template <typename T, int KF, int VF, int G, int HT> hipError_t token_of(const MxTokenCall &p, hipStream_t s) {
+  constexpr int most = token_lds<G, HT>(16 * HT);
+  static_assert(most <= 80 * 1024, "LDS of two workgroups of a CU");
+  const int lds = token_lds<G, HT>(std::min(p.G, 16 * HT));
+  if (lds > 64 * 1024) {  // sixteen heads of more than 224 features, or 32 of more than 96: each device is told once
     static std::atomic<uint64_t> told{0};
     int device = 0;
     hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return e;
     const uint64_t bit = 1ull << (device & 63);
     if (device > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
-      e = hipFuncSetAttribute((const void *)k_mx_token<T, G, KF, VF>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+      e = hipFuncSetAttribute((const void *)k_mx_token<T, G, KF, VF, HT>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
       if (e != hipSuccess) return e;
       told.fetch_or(bit, std::memory_order_relaxed);
     }
   }
-  k_mx_token<T, G, KF, VF><<<(unsigned)p.m.c.n_requests * p.m.c.n_kv_heads * p.head_tiles * p.parts, kThreads, lds, s>>>(p);
+  k_mx_token<T, G, KF, VF, HT><<<(unsigned)p.m.c.n_requests * p.m.c.n_kv_heads * p.head_tiles * p.parts, kThreads, lds, s>>>(p);
   return hipGetLastError();
+}
+
+template <typename T, int KF, int VF, int G> hipError_t token_tiles(const MxTokenCall &p, hipStream_t s) {
+  if constexpr (mx_token_two_tiles(G, sizeof(T) == 4))
+    if (p.tiles == 2) return token_of<T, KF, VF, G, 2>(p, s);
+  return token_of<T, KF, VF, G, 1>(p, s);
 }
 
 }  // namespace
 
 template <typename T, int KF, int VF> hipError_t mx_token(const MxTokenCall &p, hipStream_t s) {
   switch (p.m.groups) {
-    case 1: return token_of<T, KF, VF, 1>(p, s);
-    case 2: return token_of<T, KF, VF, 2>(p, s);
-    case 3: return token_of<T, KF, VF, 3>(p, s);
-    case 4: return token_of<T, KF, VF, 4>(p, s);
-    case 5: return token_of<T, KF, VF, 5>(p, s);
-    case 6: return token_of<T, KF, VF, 6>(p, s);
-    case 7: return token_of<T, KF, VF, 7>(p, s);
-    default: return token_of<T, KF, VF, 8>(p, s);
+    case 1: return token_tiles<T, KF, VF, 1>(p, s);
+    case 2: return token_tiles<T, KF, VF, 2>(p, s);
+    case 3: return token_tiles<T, KF, VF, 3>(p, s);
+    case 4: return token_tiles<T, KF, VF, 4>(p, s);
+    case 5: return token_tiles<T, KF, VF, 5>(p, s);
+    case 6: return token_tiles<T, KF, VF, 6>(p, s);
+    case 7: return token_tiles<T, KF, VF, 7>(p, s);
+    default: return token_tiles<T, KF, VF, 8>(p, s);
   }
 }
 

@@ -8,11 +8,11 @@ int main() {
   char what[16];
   while (scanf("%15s", what) == 1) {
     long long a, b, c, d, e;
-    int f;
+    int f, g, h;
     if (!strcmp(what, "token")) {
-      if (scanf("%lld %lld %lld %lld %lld %d", &a, &b, &c, &d, &e, &f) != 6) return 1;
-      const hyp::MxTokenPlan t = hyp::mx_token_plan(a, b, c, d, e, f != 0);
-      printf("%d %d %d\n", t.unit, t.units, t.parts);
+      if (scanf("%lld %d %lld %lld %lld %lld %d %d", &a, &f, &b, &c, &d, &e, &g, &h) != 8) return 1;
+      const hyp::MxTokenPlan t = hyp::mx_token_plan(a, f, b, c, d, e, g, h != 0);
+      printf("%d %d %d %d %d\n", t.tiles, t.head_tiles, t.unit, t.units, t.parts);
     } else if (!strcmp(what, "scores")) {
       if (scanf("%lld %lld", &a, &b) != 2) return 1;
       const int turns = hyp::mx_score_turns(a, b);

@@ -59,6 +59,19 @@ def test_groups_of_heads(nkv, heads, dtype):
     check(pr, rows(pr, heads, dtype))
 
 
+@pytest.mark.parametrize("formats", FORMATS)
+@pytest.mark.parametrize("group,d", [(17, 128), (24, 64), (32, 96), (33, 32), (71, 80)])
+def test_wide_groups_over_enough_keys_for_two_tiles_of_heads(group, d, formats):
+    # listed blocks, of which most are none: launches are cut by what may be listed, and the reference has few keys to look at
+    held, block = [4200, 70, 0, 4095], 256
+    pr = Problem(15, held, nkv=1, d=d, formats=formats, dtype=BF, block=block, most=8192).fill()
+    q, listed = rows(pr, group, BF), 512 * 256 // (4 * -(-group // 32)) // block + 1
+    lists = [[[i % 17 if i % 40 == 3 and held[b] else -1 for i in range(listed)]] for b in range(4)]
+    check(pr, q, lists, cap=20.0, slopes=[0.01 * (h % 5) for h in range(group)])
+    long = Problem(16, [3000], nkv=1, d=d, formats=formats, dtype=BF, most=132000, layout="pages", page=1024).fill()
+    check(long, rows(long, group, BF))
+
+
 @pytest.mark.parametrize("layout", ["slab", "pages", "inner"])
 @pytest.mark.parametrize("held", [[0, 1, 2, 15], [16, 17, 31, 32], [33, 47, 48, 49], [127, 128, 129, 0], [300, 1, 255, 257]])
 def test_lengths_and_layouts(held, layout):

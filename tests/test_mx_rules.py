@@ -32,9 +32,15 @@ def ask(tmp_path_factory):
 
 def test_token_parts(ask):
     rng = random.Random(1)
-    cases = [(rng.choice((1, 2, 8, 64, 255, 320, 5000, 1 << 23)), rng.choice((1, 15, 17, 256, 1023, 1024, 9000, 131072, (1 << 30) - 1)), rng.choice((16, 32, 48, 128, 1 << 20)),
-              rng.choice((0, 0, 16, 32, 256)), rng.choice((34, 66, 136, 200, 264, 528)), rng.choice((0, 1))) for _ in range(600)]
-    for (unit, units, parts), (items, keys, page, block, size, f32) in zip(ask([("token " + " ".join(map(str, c))) for c in cases]), cases):
+    cases = []
+    for _ in range(900):
+        features, formats = rng.choice((1, 2, 3, 4, 5, 8)), rng.choice((34, 50, 66))
+        cases.append((rng.choice((1, 2, 8, 64, 255, 320, 5000, 1 << 23)), rng.choice((1, 4, 16, 17, 24, 71, 256)), rng.choice((1, 15, 17, 256, 1023, 1024, 9000, 131072, (1 << 30) - 1)),
+                      rng.choice((16, 32, 48, 128, 1 << 20)), rng.choice((0, 0, 16, 32, 256)), features * formats, features, rng.choice((0, 1))))
+    for (tiles, head_tiles, unit, units, parts), (pairs, group, keys, page, block, _, features, f32) in zip(ask([("token " + " ".join(map(str, c))) for c in cases]), cases):
+        assert tiles in (1, 2) and 16 * tiles * head_tiles >= group > 16 * tiles * (head_tiles - 1)
+        assert tiles == 1 or (group > 16 and features <= 4 and not f32)    # the kernels there are
+        items = pairs * head_tiles
         assert unit == (4 if page % 32 or block == 16 else 5)             # a unit lies in one page and block
         assert 1 <= units <= 256 and units % 8 == 0
         assert units * parts << unit >= keys > units * (parts - 1) << unit  # all keys have a part, and every part has keys
@@ -69,7 +75,7 @@ def test_every_block_that_rows_touch_has_a_tile(ask):
 
 def test_kernels_do_not_spill(kernels):  # noqa: F811
     found = {name: k for name, k in kernels.items() if re.search(r"k_mx_", name)}
-    assert sum("k_mx_token" in name for name in found) == 64   # two types, eight sizes, two formats of either
+    assert sum("k_mx_token" in name for name in found) == 64 + 16   # two types, eight sizes, two formats of either; up to 128 bf16 features for two tiles of heads
     for name, k in found.items():
         assert k["scratch"] == 0 and k["spilled"] == 0, (name, k)
         if "k_mx_token" in name and "k_mx_tokenIfLi7" not in name and "k_mx_tokenIfLi8" not in name:
