@@ -68,33 +68,40 @@ __device__ __forceinline__ double element(const uint4 &v, int i, bool there) {
 // The vector unit has neither the time for that (a conversion of a float takes four ordinary instructions': 22 us for 64 caches of up to 2048
 // blocks of 128 features) nor for the sums over lanes; the matrix unit's 4 x 4 x 4 product does both: 16 blocks on the M axis of its four
 // batches, 4 heads on the N axis, lane l holds blocks l % 16 and heads l % 4 in four pieces of features, l / 16 of them, and gets the score of
-// block 4 (l / 4 % 4) + l / 16 with head l % 4.  N: pieces of eight features of a lane at a time.
-constexpr int kTurns = 4;
-template <typename T, int N, bool WIDE, typename Put> __device__ __forceinline__ void score_blocks(const MxSelectCall &p, int b, int kvh, int first, int turns, int end, Put &&put) {
+// block 4 (l / 4 % 4) + l / 16 with head l % 4.  N pieces of eight features of a lane, 64 features of a row, are held at a time: with 128 two waves
+// a SIMD instead of three (23.5 us a call, 22.7).
+constexpr int kTurns = 4, N = 2;
+struct Places { int page[kTurns], in[kTurns]; };  // of the blocks of a lane
+__device__ __forceinline__ Places places_of(const MxSelectCall &p, int b, int first, int turns) {
+  const hyp_mx_cache_t &c = p.m.c;
+  Places at;
+  first += 16 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + (threadIdx.x & 15);
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    at.page[t] = b;
+    at.in[t] = min(first + 64 * min(t, turns - 1), p.most_blocks - 1);  // there is room for these, held or not
+  }
+  if (c.page_table) {
+    const int s = p.m.shift - p.m.block_shift;  // log2(blocks of a page)
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) at.page[t] = c.page_table[(int64_t)b * c.pages_per_request + (at.in[t] >> s)];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) at.in[t] &= (1 << s) - 1;
+  }
+  return at;
+}
+
+template <typename T, bool WIDE, typename Put>
+__device__ __forceinline__ void score_blocks(const MxSelectCall &p, const Places &where, int b, int kvh, int first, int turns, int end, Put &&put) {
   const hyp_mx_cache_t &c = p.m.c;
   const int lane = threadIdx.x & 63, chunk = lane >> 4, d = c.head_dim, group = p.q.n_q_heads / c.n_kv_heads;
   first += 16 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (first >= end) return;
   const bf16_t *lo = (const bf16_t *)c.lo, *hi = (const bf16_t *)c.hi;
-  int page[kTurns], in[kTurns];
   int64_t at[kTurns];
 #pragma unroll
-  for (int t = 0; t < kTurns; ++t) {
-    page[t] = b;
-    in[t] = min(first + 64 * min(t, turns - 1) + (lane & 15), end - 1);
-  }
-  if (c.page_table) {
-    const int s = p.m.shift - p.m.block_shift;  // log2(blocks of a page)
-#pragma unroll
-    for (int t = 0; t < kTurns; ++t) page[t] = c.page_table[(int64_t)b * c.pages_per_request + (in[t] >> s)];
-#pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-      page[t] = mx_clamped(page[t], 0, c.n_pages - 1);
-      in[t] &= (1 << s) - 1;
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < kTurns; ++t) at[t] = page[t] * c.bound_page_stride + kvh * c.bound_head_stride + in[t] * c.bound_block_stride;
+  for (int t = 0; t < kTurns; ++t)
+    at[t] = (c.page_table ? mx_clamped(where.page[t], 0, c.n_pages - 1) : b) * c.bound_page_stride + kvh * c.bound_head_stride + where.in[t] * c.bound_block_stride;
   for (int g0 = 0; g0 < group; g0 += kHeads) {
     const T *row = (const T *)p.q.q + b * p.q.q_row_stride + (kvh * group + min(g0 + (lane & 3), group - 1)) * p.q.q_head_stride;
     double up[kTurns], down[kTurns];     // sums over features whose largest numbers count, and whose least do
@@ -150,12 +157,13 @@ template <typename T, int N, bool WIDE, typename Put> __device__ __forceinline__
   }
 }
 
-template <typename T, int N, bool WIDE> __global__ void __launch_bounds__(kThreads, 2) k_mx_scores(const MxSelectCall p, int tiles, int turns) {
+template <typename T, bool WIDE> __global__ void __launch_bounds__(kThreads, 2) k_mx_scores(const MxSelectCall p, int tiles, int turns) {
   const int tile = blockIdx.x % tiles, pair = blockIdx.x / tiles, b = pair / p.m.c.n_kv_heads, kvh = pair % p.m.c.n_kv_heads;
+  const Places where = places_of(p, b, tile * 64 * turns, turns);  // waits for no length
   const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
   if (count <= p.keep) return;
   u64 *order = p.order + (int64_t)pair * p.most_blocks;
-  score_blocks<T, N, WIDE>(p, b, kvh, tile * 64 * turns, turns, min(count, (tile + 1) * 64 * turns), [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
+  score_blocks<T, WIDE>(p, where, b, kvh, tile * 64 * turns, turns, min(count, (tile + 1) * 64 * turns), [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
 }
 
 // sum of v over the threads before this one, and over all; scratch: one int a wave
@@ -189,13 +197,16 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) k_mx_choose(co
   __shared__ u64 ends[2], cand[kMostCandidates];
   __shared__ int cand_at[kMostCandidates];
   const int pair = blockIdx.x, b = pair / p.m.c.n_kv_heads, tid = threadIdx.x, lane = tid & 63, K = p.keep;
+  const u64 *order = p.order + (int64_t)pair * p.most_blocks;
+  u64 held[kItems];                      // the first orders, which wait for no length
+#pragma unroll
+  for (int x = 0; x < kItems; ++x) held[x] = order[min(tid * kItems + x, p.most_blocks - 1)];
   const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
   int *out = p.blocks + (int64_t)pair * K;
   if (count <= K) {
     for (int r = tid; r < K; r += THREADS) out[r] = r < count ? r : -1;
     return;
   }
-  const u64 *order = p.order + (int64_t)pair * p.most_blocks;
   const int newest = count - p.recent;
   // a thread has runs of kItems blocks, so that counts in the order of threads are counts in the order of blocks
   constexpr int STEP = THREADS * kItems;
@@ -205,7 +216,7 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) k_mx_choose(co
 #pragma unroll
     for (int x = 0; x < kItems; ++x) {
       const int i = base + tid * kItems + x;
-      u[x] = i >= count ? 0 : (i < p.sink || i >= newest) ? ~0ull : order[i];
+      u[x] = i >= count ? 0 : (i < p.sink || i >= newest) ? ~0ull : base == 0 ? held[x] : order[i];
     }
   };
   auto each = [&](auto &&f) {  // f(block, its order), for those with a score of their own
@@ -338,17 +349,18 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) k_mx_choose(co
 }
 
 // The same for requests of up to 256 blocks, scores and choice in one launch: a block is taken if fewer than `keep` come before it.
-template <typename T, int N, bool WIDE> __global__ void __launch_bounds__(kThreads, 2) k_mx_select_small(const MxSelectCall p) {
+template <typename T, bool WIDE> __global__ void __launch_bounds__(kThreads, 2) k_mx_select_small(const MxSelectCall p) {
   __shared__ u64 order[kMxSmallBlocks];
   __shared__ int scratch[kThreads / 64];
   const int pair = blockIdx.x, b = pair / p.m.c.n_kv_heads, kvh = pair % p.m.c.n_kv_heads, tid = threadIdx.x, K = p.keep;
+  const Places where = places_of(p, b, 0, kTurns);
   const int count = (int)(((int64_t)mx_len(p.m.c, b) + (1 << p.m.block_shift) - 1) >> p.m.block_shift);
   int *out = p.blocks + (int64_t)pair * K;
   if (count <= K) {
     for (int r = tid; r < K; r += kThreads) out[r] = r < count ? r : -1;
     return;
   }
-  score_blocks<T, N, WIDE>(p, b, kvh, 0, kTurns, count, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
+  score_blocks<T, WIDE>(p, where, b, kvh, 0, kTurns, count, [&](int i, u64 v, bool more) { order[i] = more ? max(order[i], v) : v; });
   __syncthreads();
   if (tid >= count) order[tid] = 0;
   else if (tid < p.sink || tid >= count - p.recent) order[tid] = ~0ull;
@@ -365,14 +377,14 @@ template <typename T, int N, bool WIDE> __global__ void __launch_bounds__(kThrea
   if (taken) out[at] = tid;
 }
 
-template <typename T, int N, bool WIDE> hipError_t select(const MxSelectCall &p, hipStream_t s) {
+template <typename T, bool WIDE> hipError_t select(const MxSelectCall &p, hipStream_t s) {
   const unsigned pairs = (unsigned)p.m.c.n_requests * p.m.c.n_kv_heads;
   if (mx_select_once(p.most_blocks, p.keep)) {
-    k_mx_select_small<T, N, WIDE><<<pairs, kThreads, 0, s>>>(p);
+    k_mx_select_small<T, WIDE><<<pairs, kThreads, 0, s>>>(p);
     return hipGetLastError();
   }
   const int turns = mx_score_turns(pairs, p.most_blocks), tiles = mx_score_tiles(p.most_blocks, turns);
-  k_mx_scores<T, N, WIDE><<<pairs * tiles, kThreads, 0, s>>>(p, tiles, turns);
+  k_mx_scores<T, WIDE><<<pairs * tiles, kThreads, 0, s>>>(p, tiles, turns);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;  // the choice goes by the scores
   if (p.most_blocks <= kMxChooseBlocks) k_mx_choose<512><<<pairs, 512, 0, s>>>(p);
@@ -383,8 +395,7 @@ template <typename T, int N, bool WIDE> hipError_t select(const MxSelectCall &p,
 }  // namespace
 
 template <typename T> hipError_t mx_select(const MxSelectCall &p, hipStream_t s) {
-  if (p.wide) return p.m.c.head_dim <= 64 ? select<T, 2, true>(p, s) : select<T, 4, true>(p, s);
-  return select<T, 2, false>(p, s);
+  return p.wide ? select<T, true>(p, s) : select<T, false>(p, s);
 }
 
 template hipError_t mx_select<float>(const MxSelectCall &, hipStream_t);
