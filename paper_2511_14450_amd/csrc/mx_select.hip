@@ -69,7 +69,8 @@ __device__ __forceinline__ double element(const uint4 &v, int i, bool there) {
 // blocks of 128 features) nor for the sums over lanes; the matrix unit's 4 x 4 x 4 product does both: 16 blocks on the M axis of its four
 // batches, 4 heads on the N axis, lane l holds blocks l % 16 and heads l % 4 in four pieces of features, l / 16 of them, and gets the score of
 // block 4 (l / 4 % 4) + l / 16 with head l % 4.  N pieces of eight features of a lane, 64 features of a row, are held at a time: with 128 two waves
-// a SIMD instead of three (23.5 us a call, 22.7).
+// a SIMD instead of three (23.5 us a call, 22.7).  Those 64 caches, 53 MB of bounds, take 15.5 us: without the reads 10, of which the products
+// and conversions are 6; what is left is waiting, for all workgroups run at once and each goes through four turns.
 constexpr int kTurns = 4, N = 2;
 struct Places { int page[kTurns], in[kTurns]; };  // of the blocks of a lane
 __device__ __forceinline__ Places places_of(const MxSelectCall &p, int b, int first, int turns) {
@@ -189,7 +190,8 @@ template <int WAVES> __device__ __forceinline__ int before_me(int v, int *scratc
 }
 
 // One request and KV head with more blocks than are kept.  Scores are sorted into kBins bins between the least and the largest; the bin in which
-// the last one falls that is taken is cut into as many again until it holds few, which are then ranked one by one.
+// the last one falls that is taken is cut into as many again until it holds few, which are then ranked one by one.  Barriers bound it, some fifteen:
+// 7 us for 64 pairs of up to 2048 blocks (88 where up to 1024 were ranked one by one).
 template <int THREADS> __global__ void __launch_bounds__(THREADS) k_mx_choose(const MxSelectCall p) {
   constexpr int WAVES = THREADS / 64, kMostCandidates = THREADS / 8;
   constexpr int kBins = 2 * THREADS, kBits = 31 - __builtin_clz(kBins);  // two bins a thread

@@ -7,6 +7,13 @@
 // keys are taken in the same order: a lane holds 2 to 8 adjacent features of those eight keys, converted as pairs of features and exchanged to
 // pairs of keys.  Codes go from memory to registers; nothing of the keys passes through LDS.  The codes' numbers are bf16 as they stand, so that
 // products of bf16 rows are exact; float rows and probabilities are three bf16 that add up to them.
+//
+// Bytes bound 8 bits: 8 x 32768 keys of 8 heads of 128 features, scores capped and falling with the distance, 92 us, of which the keys take 86 - 88 (6.3 -
+// 6.4 TB/s; a streaming read reaches 6.45) and the join 4.8.  4 bits have half as many and are bound by the issue of instructions and by waiting: 54 us,
+// 5.3 TB/s.  What it took: no clamped places in the loop (whole runs lie in the room; lengths count where codes are used), bytes to a unit of keys
+// in LDS, where 64-bit products on the scalar unit were (together 105 -> 96), streaming loads (-7 us; a cache that fits the memory-side one, of
+// 19 MB, takes 1 us more), the next pair of runs requested before one is worked on (4 bits: 59 -> 54; without it, at four waves a SIMD, 8 bits
+// are as fast), one workgroup a CU for 8 bits.  Eight waves a workgroup were slower (32 requests of 101 - 608 keys: 18.7 instead of 12).
 #pragma once
 
 #include <atomic>
@@ -20,7 +27,6 @@ namespace hyp {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr bool kNtK = true, kNtV = true;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFollow = 8.0f;     // the running maximum moves when a score passes it by more than 2^8
 constexpr float kLowest = -3.402823466e38f;  // the maximum of no score: finite, so that a score of -infinity has the weight 0 beside it
@@ -44,8 +50,8 @@ constexpr int piece_bytes(int format, int feats) { return format == HYP_E4M3 ? f
 
 typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
-template <int BYTES, bool NT> __device__ __forceinline__ void load_bytes(const uint8_t *p, unsigned *w) {
-  auto get = [](auto *at) { return NT ? __builtin_nontemporal_load(at) : *at; };
+template <int BYTES> __device__ __forceinline__ void load_bytes(const uint8_t *p, unsigned *w) {
+  auto get = [](auto *at) { return __builtin_nontemporal_load(at); };  // read once, and more of them than the caches hold
   if constexpr (BYTES == 16) {
     const u32x4_t x = get((const u32x4_t *)p);
     w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
@@ -224,9 +230,9 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
       // the pieces behind the first may be shorter, and a lane's place in them with it
       const unsigned at = k_at - (unsigned)((piece_bytes(KF, P.at[0].feats) - bytes) * quarter);
       const uint8_t *from = k + piece_bytes(KF, P.at[i].base) + at;
-      if (bytes == 16) load_bytes<16, kNtK>(from, &r.k[w]);
-      else if (bytes == 8) load_bytes<8, kNtK>(from, &r.k[w]);
-      else load_bytes<4, kNtK>(from, &r.k[w]);
+      if (bytes == 16) load_bytes<16>(from, &r.k[w]);
+      else if (bytes == 8) load_bytes<8>(from, &r.k[w]);
+      else load_bytes<4>(from, &r.k[w]);
       w += words(bytes);
       r.ks[i] = ks[ks_at[i]];
     }
@@ -238,10 +244,10 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
         constexpr auto P = VP;
         const int bytes = piece_bytes(VF, P.at[i].feats);
         const uint8_t *from = v + piece_bytes(VF, P.at[i].base) + (v_at[j] + (unsigned)(bytes * col));
-        if (bytes == 8) load_bytes<8, kNtV>(from, &r.v[j][w]);
-        else if (bytes == 4) load_bytes<4, kNtV>(from, &r.v[j][w]);
-        else if (bytes == 2) load_bytes<2, kNtV>(from, &r.v[j][w]);
-        else load_bytes<1, kNtV>(from, &r.v[j][w]);
+        if (bytes == 8) load_bytes<8>(from, &r.v[j][w]);
+        else if (bytes == 4) load_bytes<4>(from, &r.v[j][w]);
+        else if (bytes == 2) load_bytes<2>(from, &r.v[j][w]);
+        else load_bytes<1>(from, &r.v[j][w]);
         w += words(bytes);
       }
     }
@@ -272,6 +278,11 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
           for (int t = 0; t < QP; ++t) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[h][t][step], s[h], 0, 0, 0);
       }
     }
+  }
+
+  __device__ __forceinline__ void clear_behind(f32x4_t &s, const Run &r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = 4 * quarter + i < r.valid ? s[i] : 0.f;
   }
 
   // Scores of keys first + 4 quarter + i as exponents of two, -infinity where there is no such key; raw: all lie where the polynomial of a cap holds
@@ -311,6 +322,9 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
     bf16x8_t prob[HT][QP];
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
+      // what is behind the last key has no part in which form of the cap is taken either, whose roundings differ
+      if (a.valid < 16) clear_behind(s0[h], a);
+      if (b.valid < 16) clear_behind(s1[h], b);
       bool raw = false;
       if (p.cap2 != 0.f) {
         const float far = fmaxf(fmaxf(fmaxf(fabsf(s0[h][0]), fabsf(s0[h][1])), fmaxf(fabsf(s0[h][2]), fabsf(s0[h][3]))),

@@ -176,6 +176,27 @@ def test_keys_that_are_not_seen_have_no_influence_whatever_they_hold(dtype):
     assert hyp.mx_token(pr.cache, hyp.AttnRule(0.125), q.cuda())[0][1].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_what_lies_behind_the_last_key_does_not_move_a_bit(dtype):
+    # zeros, random bytes and the largest numbers there, which a cap would treat in its form for large scores
+    got = []
+    for behind in (0, None, 0x7e):
+        pr = Problem(17, [37, 75, 5], d=64, formats=("e4m3", "e4m3"), dtype=dtype, block=0, most=96).fill()
+        if behind is not None:
+            for b, h in enumerate(pr.held):
+                for t in (pr.k, pr.v):
+                    t[b, :, h:] = behind
+                for t in (pr.ks, pr.vs):
+                    t[b, :, :, h:] = 200 if behind else 127
+        q = torch.randn((3, 4, 64), generator=torch.Generator().manual_seed(18)).to(dtype)
+        for cap in (0.0, 40.0):
+            rule = hyp.AttnRule(0.125, cap=cap, slopes=torch.tensor([0.3, 0.1, 0.01, 0.77]).cuda())
+            got.append(hyp.mx_token(pr.cache, rule, q.cuda()))
+    for out, lse in got[2:]:
+        assert any(torch.equal(out, a) and torch.equal(lse, b) for a, b in got[:2])
+    assert all(torch.equal(x, y) for i in (0, 1) for x, y in zip(got[i], got[i + 4]))
+
+
 def test_rows_of_infinities_and_of_scores_beyond_floats():
     pr = Problem(12, [50], nkv=1, d=32, formats=("e4m3", "e4m3"), dtype=F32).fill()
     q = rows(pr, 3, F32)
