@@ -421,6 +421,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && G > 6 ? 1 : 2) k_mx_token(const MxTokenCall p) {
   using Tk = Token<T, G, KF, VF, HT>;
   extern __shared__ char lds[];
+  __shared__ int held[kWaves];           // units up to the last one of each wave's that holds keys
   Place *places = (Place *)lds;
   const hyp_mx_cache_t &c = p.m.c;
   const int part = blockIdx.x % p.parts, item = blockIdx.x / p.parts, ht = item % p.head_tiles, pair = item / p.head_tiles;
@@ -438,16 +439,20 @@ template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bo
     slope2[h] = p.slopes && head < p.G ? p.slopes[qh] * kLog2e : 0.f;
   }
   // all units that the part can have, so that nothing waits for the length; those behind the last one that holds keys are left out below
-  for (int i = threadIdx.x; i < min(p.units, most - u0); i += kThreads) {
-    const int u = u0 + i;
+  static_assert(kMxMostUnits <= kThreads, "a unit a thread");
+  int end = min(p.units, most - u0);
+  bool holds = false;                    // of listed ones
+  if ((int)threadIdx.x < end) {
+    const int i = threadIdx.x, u = u0 + i;
     Place at = {};
     at.first = u << p.unit;
     if (p.listed) {
       const int block = p.blocks[(int64_t)pair * p.listed + (u >> per)];
-      const bool held = len > 0 && block >= 0 && block <= (len - 1) >> p.m.block_shift;
-      at.first = held ? (block << p.m.block_shift) + ((u & ((1 << per) - 1)) << p.unit) : 0;  // else a place that may be read
-      at.valid = held ? mx_clamped(len - at.first, 0, unit) : 0;
+      const bool its = len > 0 && block >= 0 && block <= (len - 1) >> p.m.block_shift;
+      at.first = its ? (block << p.m.block_shift) + ((u & ((1 << per) - 1)) << p.unit) : 0;  // else a place that may be read
+      at.valid = its ? mx_clamped(len - at.first, 0, unit) : 0;
       if (at.valid == 0) at.first = 0;
+      holds = at.valid > 0;
     }
     int page = b, in = at.first;
     if (c.page_table) {
@@ -460,12 +465,20 @@ template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bo
     at.vs = page * c.v_scale_page_stride + kvh * c.v_scale_head_stride + in;
     places[i] = at;
   }
-  int end = min(p.units, most - u0);
-  if (!p.listed) {
+  if (p.listed) {
+    const unsigned long long votes = __ballot(holds);
+    if (t.lane == 0) held[wave] = votes ? 64 * wave + 64 - __clzll((long long)votes) : 0;
+  } else {
     end = min(end, (int)(((int64_t)len + unit - 1) >> p.unit) - u0);
     if (end <= 0 && part > 0) return;    // the join does not look at it
   }
   __syncthreads();
+  if (p.listed) {
+    end = held[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) end = max(end, held[w]);
+    end = __builtin_amdgcn_readfirstlane(end);
+  }
   t.aim();
   t.clear();
   auto fetch = [&](typename Tk::Run &a, typename Tk::Run &z, int i) {
