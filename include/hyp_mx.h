@@ -34,8 +34,9 @@
  * mx_last_error().  Values on the device are not trusted: lengths are cut to 0..most, row ranges to the
  * rows there are, page numbers to the pool, and blocks that a request does not hold are not read, so that
  * wrong ones give wrong numbers but no access outside the tensors.  The calls keep no state; any number
- * of threads and streams may make them, each with a workspace of its own.  Calls that write a request's cache and calls that read it are
- * the caller's to order, as are two requests whose tables name the same page.
+ * of threads and streams may make them, each with a workspace of its own.  Calls that write a request's
+ * cache and calls that read it are the caller's to order, as are two requests whose tables name the same
+ * page.
  */
 #ifndef HYP_MX_H
 #define HYP_MX_H
@@ -112,8 +113,8 @@ typedef struct {
 } hyp_mx_q_t;
 
 /* Quantise rows into the cache, and move bounds along where the cache has them.  Rows for keys below 0
- * or from `most` on are left out (a request with more rows than keys), rows and slots that no request
- * names stay as they are.
+ * are left out (a request with more rows than keys; a length above `most` counts as `most`), rows and
+ * slots that no request names stay as they are.
  * Errors of all calls: HYP_EINVAL (null pointer, bad enum or value, misaligned, results that share memory
  * by a stride of 0), HYP_ESHAPE (sizes that do not go together), HYP_ENOMEM (workspace too small),
  * HYP_EDEVICE. */
