@@ -421,7 +421,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && G > 6 ? 1 : 2) k_mx_token(const MxTokenCall p) {
   using Tk = Token<T, G, KF, VF, HT>;
   extern __shared__ char lds[];
-  __shared__ int held[kWaves];           // units up to the last one of each wave's that holds keys
+  __shared__ int held[kWaves];           // units up to the last one that holds keys, among each wave's
   Place *places = (Place *)lds;
   const hyp_mx_cache_t &c = p.m.c;
   const int part = blockIdx.x % p.parts, item = blockIdx.x / p.parts, ht = item % p.head_tiles, pair = item / p.head_tiles;
@@ -602,9 +602,10 @@ template <int G, int HT> constexpr int token_lds(int heads) {
 
 template <typename T, int KF, int VF, int G, int HT> hipError_t token_of(const MxTokenCall &p, hipStream_t s) {
   constexpr int most = token_lds<G, HT>(16 * HT);
-  static_assert(most <= 80 * 1024, "LDS of two workgroups of a CU");
+  constexpr int own = kWaves * 4;        // what the kernel has beside it
+  static_assert(most + own <= 80 * 1024, "LDS of two workgroups of a CU");
   const int lds = token_lds<G, HT>(std::min(p.G, 16 * HT));
-  if (lds > 64 * 1024) {  // sixteen heads of more than 224 features, or 32 of more than 96: each device is told once
+  if (lds + own > 64 * 1024) {  // sixteen heads of more than 224 features, or 32 of more than 96: each device is told once
     static std::atomic<uint64_t> told{0};
     int device = 0;
     hipError_t e = hipGetDevice(&device);
