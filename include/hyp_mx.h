@@ -144,8 +144,8 @@ HYP_API hyp_status_t mx_select(const hyp_mx_cache_t *cache, const hyp_mx_q_t *q,
  *           the request (-1) is left out, one that stands there twice counts twice.  null with listed 0: all keys.
  *   workspace  >= mx_token_workspace_bytes(), 16-byte aligned; may be null where that is 0
  * Sums and the softmax are held in 32-bit floats.  Products are exact but for the probabilities that multiply
- * values: next to bf16 rows these are rounded to bf16 once (their sum is not), next to float rows they
- * and the rows are taken in three parts of 8 bits, which hold them whole. */
+ * values: next to bf16 rows these are taken as two bf16 (off by at most 2^-16 of themselves; their sum is not
+ * rounded), next to float rows they and the rows are taken in three parts of 8 bits, which hold them whole. */
 HYP_API size_t mx_token_workspace_bytes(const hyp_mx_cache_t *cache, const hyp_mx_q_t *q, int32_t listed);
 HYP_API hyp_status_t mx_token(const hyp_mx_cache_t *cache, const hyp_attn_rule_t *rule, const hyp_mx_q_t *q, const int32_t *blocks, int32_t listed,
                               const hyp_attn_out_t *out, void *workspace, size_t workspace_bytes, void *hip_stream);

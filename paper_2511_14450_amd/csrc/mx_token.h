@@ -6,7 +6,9 @@
 // cap, distance and mask stay in its four lanes, and its probabilities are the operand of O^T += V^T P^T as they stand, if that product's
 // keys are taken in the same order: a lane holds 2 to 8 adjacent features of those eight keys, converted as pairs of features and exchanged to
 // pairs of keys.  Codes go from memory to registers; nothing of the keys passes through LDS.  The codes' numbers are bf16 as they stand, so that
-// products of bf16 rows are exact; float rows and probabilities are three bf16 that add up to them.
+// products of bf16 rows are exact; float rows and the probabilities beside them are three bf16 that add up to them.  Beside bf16 rows a probability is
+// the sum of two, which hold it to 2^-16: as one, results were 2.0e-3 from the formula in 64 bits where rounding the results to bf16 costs
+// 1.6e-3 - 1.7e-3, and sums in which values cancel were off by as much as their terms' 2^-8.
 //
 // Bytes bound 8 bits: 8 x 32768 keys of 8 heads of 128 features, scores capped and falling with the distance, 92 us, of which the keys take 86 - 88 (6.3 -
 // 6.4 TB/s; a streaming read reaches 6.45) and the join 4.8.  4 bits have half as many and are bound by the issue of instructions and by waiting: 54 us,
@@ -73,11 +75,15 @@ __device__ __forceinline__ bf16x8_t as_bf16x8(const unsigned (&w)[4]) {
   return __builtin_bit_cast(bf16x8_t, x);
 }
 
-// x as one bf16 (rounded), or as the sum of three: the first and the second are x and the rest cut to 8 bits, the third is what is left.
+// x as the sum of two bf16, x and the rest rounded, or of three: the first and the second are x and the rest cut to 8 bits, the third is what is left.
 template <int PARTS> __device__ __forceinline__ void split8(const float (&x)[8], bf16x8_t (&out)[PARTS]) {
-  if constexpr (PARTS == 1) {
+  static_assert(PARTS == 2 || PARTS == 3, "two or three");
+  if constexpr (PARTS == 2) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[0][i] = (__bf16)x[i];
+    for (int i = 0; i < 8; ++i) {
+      out[0][i] = (__bf16)x[i];
+      out[1][i] = (__bf16)(x[i] - (float)out[0][i]);
+    }
   } else {
     unsigned w[3][4];
 #pragma unroll
@@ -104,7 +110,7 @@ template <int PARTS> __device__ __forceinline__ void split8(const float (&x)[8],
 
 // HT: tiles of 16 query heads of a wave
 template <typename T, int G, int KF, int VF, int HT> struct Token {
-  static constexpr int QP = sizeof(T) == 4 ? 3 : 1;  // parts of rows and probabilities
+  static constexpr int QP = sizeof(T) == 4 ? 3 : 1, PP = sizeof(T) == 4 ? 3 : 2;  // parts of rows, and of probabilities
   static constexpr Pieces<G, KF, true> KP{};
   static constexpr Pieces<G, VF, false> VP{};
   static constexpr int VW = [] { int n = 0; for (int i = 0; i < VP.n; ++i) n += words(piece_bytes(VF, VP.at[i].feats)); return n; }();
@@ -319,7 +325,7 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
     f32x4_t s0[HT], s1[HT];
     scores(a, s0);
     scores(b, s1);
-    bf16x8_t prob[HT][QP];
+    bf16x8_t prob[HT][PP];
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
       // what is behind the last key has no part in which form of the cap is taken either, whose roundings differ
@@ -351,7 +357,7 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) l[h] += x[i];
-      split8<QP>(x, prob[h]);
+      split8<PP>(x, prob[h]);
     }
     if (a.valid < 16) mend(a);
     if (b.valid < 16) mend(b);
@@ -381,7 +387,7 @@ template <typename T, int G, int KF, int VF, int HT> struct Token {
 #pragma unroll
         for (int h = 0; h < HT; ++h)
 #pragma unroll
-          for (int x = 0; x < QP; ++x) {
+          for (int x = 0; x < PP; ++x) {
             o[h][at] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), prob[h][x], o[h][at], 0, 0, 0);
             o[h][at + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), prob[h][x], o[h][at + 1], 0, 0, 0);
           }
