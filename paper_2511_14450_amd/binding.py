@@ -271,12 +271,20 @@ def stage_context_len(stage: Stage, request: int) -> int:
 
 
 def stage_export_kv(stage: Stage, layer: int, request: int):
+    """(keys, values) [context, kv heads * head_dim] of one request and block, tensors of the current stream: copied on the stage's, behind
+    what the current one holds, and complete for what follows there."""
     n = stage_context_len(stage, request)
     kvd = stage.cfg.n_kv_heads * stage.cfg.head_dim
     k = torch.empty((n, kvd), dtype=_torch_dtype(stage.cfg.dtype), device="cuda")
     v = torch.empty_like(k)
+    here = torch.cuda.current_stream()
+    aside = stage.stream.cuda_stream != here.cuda_stream
+    if aside:
+        stage.stream.wait_stream(here)  # what had this memory before may be at work on it there
     status = load_library().stage_export_kv(stage.handle, layer, request, k.data_ptr(), v.data_ptr())
     _check(status, stage.handle)
+    if aside:
+        here.wait_stream(stage.stream)
     return k, v
 
 
