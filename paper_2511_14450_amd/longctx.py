@@ -15,9 +15,10 @@ A context may also come from a stage that ran the prompts (`adopt`): its caches 
 from __future__ import annotations
 
 import argparse
+import contextlib
 import json
 import time
-from typing import Dict, Sequence
+from typing import Dict, List, Sequence
 
 import torch
 
@@ -50,12 +51,26 @@ class LongBlocks(BlockMath):
             self.page_table = self.caches[0].page_table
         self.held = [0] * n_requests   # what lens counts, on the host
 
-    def _grow(self, counts: Sequence[int]) -> None:
+    def _grown(self, held: Sequence[int], counts: Sequence[int]) -> List[int]:
         if len(counts) != self.n or min(counts) < 0:
             raise ValueError("need a number of new tokens for every request")
-        if any(h + c > self.most for h, c in zip(self.held, counts)):
+        if any(h + c > self.most for h, c in zip(held, counts)):
             raise ValueError(f"a request would hold more than {self.most} keys")
-        self.held = [h + c for h, c in zip(self.held, counts)]
+        return [h + c for h, c in zip(held, counts)]
+
+    @contextlib.contextmanager
+    def _holding(self, held: List[int], otherwise: List[int]):
+        """The requests hold so many keys, whom the caller counts in lens and writes, or so many others where that fails."""
+        self.held = held
+        try:
+            yield
+        except BaseException:
+            self.held = otherwise
+            self._count(otherwise)
+            raise
+
+    def _count(self, held: List[int]) -> None:
+        self.lens.copy_(torch.tensor(held, dtype=torch.int32))
 
     def reset(self) -> None:
         """All requests start anew."""
@@ -66,25 +81,24 @@ class LongBlocks(BlockMath):
         """Hidden states [sum(seq_lens), H] of the requests' prompts, or of their next chunks (0 tokens of some, if any), through the blocks."""
         if hidden.shape[0] != sum(seq_lens):
             raise ValueError("need as many rows as seq_lens say")
-        past = list(self.held)
-        self._grow(seq_lens)
-        self.lens.copy_(torch.tensor(self.held, dtype=torch.int32))
-        s, keys = self.shape, max(self.held)
+        past, held, s = self.held, self._grown(self.held, seq_lens), self.shape
         if hidden.shape[0] == 0:
             return hidden
-        start = torch.tensor([sum(seq_lens[:i]) for i in range(self.n + 1)], dtype=torch.int32).cuda()
-        turn = self._turn(torch.cat([torch.arange(p, p + n) for p, n in zip(past, seq_lens)]).cuda())
-        # room for what the requests hold, which all blocks use in turn
-        k = torch.empty((self.n, s.n_kv_heads, keys, s.head_dim), dtype=hidden.dtype, device="cuda")
-        v = torch.empty_like(k)
-        whole = attn.AttnCache(k, v, self.lens)
-        x = hidden
-        for w, cache in zip(self.layers, self.caches):
-            q, new_k, new_v = self._qkv(w, x, turn)
-            mx.mx_write(cache, new_k, new_v, q_start=start)
-            mx.mx_read(cache, k, v)
-            out, _ = attn.attn_prompt(whole, self.rule, q, start)
-            x = self._rest(w, x, out)
+        with self._holding(held, past):
+            self._count(held)
+            start = torch.tensor([sum(seq_lens[:i]) for i in range(self.n + 1)], dtype=torch.int32).cuda()
+            turn = self._turn(torch.cat([torch.arange(p, p + n) for p, n in zip(past, seq_lens)]).cuda())
+            # room for what the requests hold, which all blocks use in turn
+            k = torch.empty((self.n, s.n_kv_heads, max(held), s.head_dim), dtype=hidden.dtype, device="cuda")
+            v = torch.empty_like(k)
+            whole = attn.AttnCache(k, v, self.lens)
+            x = hidden
+            for w, cache in zip(self.layers, self.caches):
+                q, new_k, new_v = self._qkv(w, x, turn)
+                mx.mx_write(cache, new_k, new_v, q_start=start)
+                mx.mx_read(cache, k, v)
+                out, _ = attn.attn_prompt(whole, self.rule, q, start)
+                x = self._rest(w, x, out)
         return x
 
     def decode_step(self, hidden: torch.Tensor) -> torch.Tensor:
@@ -92,29 +106,31 @@ class LongBlocks(BlockMath):
         if hidden.shape[0] != self.n:
             raise ValueError("need one row for each request")
         turn, x = self._turn(self.lens), hidden
-        self._grow([1] * self.n)
-        self.lens += 1
-        for w, cache in zip(self.layers, self.caches):
-            q, k, v = self._qkv(w, x, turn)
-            mx.mx_write(cache, k, v)
-            blocks = mx.mx_select(cache, q, self.read_blocks, self.sink, self.recent) if self.read_blocks else None
-            out, _ = mx.mx_token(cache, self.rule, q, blocks=blocks)
-            x = self._rest(w, x, out)
+        with self._holding(self._grown(self.held, [1] * self.n), self.held):
+            self.lens += 1
+            for w, cache in zip(self.layers, self.caches):
+                q, k, v = self._qkv(w, x, turn)
+                mx.mx_write(cache, k, v)
+                blocks = mx.mx_select(cache, q, self.read_blocks, self.sink, self.recent) if self.read_blocks else None
+                out, _ = mx.mx_token(cache, self.rule, q, blocks=blocks)
+                x = self._rest(w, x, out)
         return x
 
     def adopt(self, stage: binding.Stage, l_start: int, l_end: int) -> None:
-        """The contexts of a stage's first n_requests requests, of the blocks [l_start, l_end) of the stage, which are these blocks; what was held is dropped."""
-        if l_end - l_start != len(self.layers):
-            raise ValueError("need as many blocks of the stage as there are here")
-        lens = [binding.stage_context_len(stage, b) for b in range(self.n)]
-        self.reset()
-        self._grow(lens)
-        self.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        """The contexts of a stage's first n_requests requests, of the blocks [l_start, l_end) of the stage, which are these blocks; what was held is dropped,
+        where a call is not refused."""
         s = self.shape
-        start = torch.tensor([sum(lens[:i]) for i in range(self.n + 1)], dtype=torch.int32).cuda()
-        for l, cache in zip(range(l_start, l_end), self.caches):
-            rows = [torch.cat(t).view(-1, s.n_kv_heads, s.head_dim) for t in zip(*(stage.export_kv(l, b) for b in range(self.n)))]
-            mx.mx_write(cache, *rows, q_start=start)
+        if l_end - l_start != len(self.layers) or l_start < 0 or l_end > stage.l_end - stage.l_start:
+            raise ValueError("need as many blocks of the stage as there are here")
+        if (stage.cfg.n_kv_heads, stage.cfg.head_dim) != (s.n_kv_heads, s.head_dim):
+            raise ValueError(f"need a stage of {s.n_kv_heads} KV heads of {s.head_dim} features")
+        lens = self._grown([0] * self.n, [binding.stage_context_len(stage, b) for b in range(self.n)])
+        with self._holding(lens, [0] * self.n):
+            self._count(lens)
+            start = torch.tensor([sum(lens[:i]) for i in range(self.n + 1)], dtype=torch.int32).cuda()
+            for l, cache in zip(range(l_start, l_end), self.caches):
+                rows = [torch.cat(t).view(-1, s.n_kv_heads, s.head_dim) for t in zip(*(stage.export_kv(l, b) for b in range(self.n)))]
+                mx.mx_write(cache, *rows, q_start=start)
 
     def cache_bytes(self) -> int:
         return sum(t.numel() * t.element_size() for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale, c.lo, c.hi) if t is not None)
