@@ -160,7 +160,7 @@ class MxCache:
                  page_keys: int = 0, n_pages: Optional[int] = None, lens: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None,
                  device="cuda") -> "MxCache":
         """An empty cache with memory of its own: slabs, or pages of page_keys keys (n_pages of them, by default enough for all; request b has pages
-        b * ceil(most / page_keys) on until the caller writes another table).  block_keys > 0: with bounds of such blocks.  lens, page_table: where
+        b * ceil(most / page_keys) on until the caller writes another table, and with fewer pages than that takes the caller has to give one).  block_keys > 0: with bounds of such blocks.  lens, page_table: where
         several caches, of a model's blocks, share them.  Its tensors are the attributes k, v, k_scale, v_scale, lens, page_table, lo and hi."""
         for name in (k_format, v_format):
             _need(name in MX_FORMATS, f"format: need one of {', '.join(MX_FORMATS)}")
@@ -170,6 +170,7 @@ class MxCache:
             per = -(-most // page_keys)
             slabs, room = n_requests * per if n_pages is None else n_pages, page_keys
             if table is None:
+                _need(slabs >= n_requests * per, f"n_pages: {slabs} pages are not enough for all requests, which have {n_requests * per}: give a page_table")
                 table = torch.arange(n_requests * per, dtype=torch.int32, device=device).reshape(n_requests, per)
         else:
             slabs, room = n_requests, -(-most // unit) * unit
