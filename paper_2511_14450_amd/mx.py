@@ -174,6 +174,8 @@ class MxCache:
                 table = torch.arange(n_requests * per, dtype=torch.int32, device=device).reshape(n_requests, per)
         else:
             slabs, room = n_requests, -(-most // unit) * unit
+        _need(block_keys == 0 or (16 <= block_keys <= 4096 and block_keys & (block_keys - 1) == 0 and room % block_keys == 0),
+              f"block_keys: need a power of two from 16 to 4096{f' that divides page_keys, {page_keys}' if page_keys else ''}")
         new = lambda *shape, dtype=torch.uint8: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
         k, v = (new(slabs, n_kv_heads, room, _GROUP_BYTES[MX_FORMATS[f]] * groups) for f in (k_format, v_format))
         k_scale, v_scale = (new(slabs, n_kv_heads, groups, room) for _ in range(2))
