@@ -136,28 +136,57 @@ class LongBlocks(BlockMath):
         return sum(t.numel() * t.element_size() for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale, c.lo, c.hi) if t is not None)
 
 
-def main():
-    from .chain import MODELS, _Shape, _synthetic_layer
-    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("--model", choices=sorted(MODELS), default="phi3_medium")
-    ap.add_argument("--blocks", type=int, default=2)
-    ap.add_argument("--requests", type=int, default=8)
-    ap.add_argument("--prompt", type=int, default=16384, help="tokens of each request's prompt")
-    ap.add_argument("--chunk", type=int, default=4096, help="of which so many at a time")
-    ap.add_argument("--generate", type=int, default=64)
+def _arguments(models: Sequence[str], argv=None) -> argparse.Namespace:
+    def at_least(least):
+        def number(text):
+            if (value := int(text)) < least:
+                raise argparse.ArgumentTypeError(f"{value} is less than {least}")
+            return value
+        return number
+
+    ap = argparse.ArgumentParser(prog="python -m paper_2511_14450_amd.longctx", description=__doc__.split("\n\n")[0])
+    ap.add_argument("--model", choices=models, default="phi3_medium")
+    ap.add_argument("--blocks", type=at_least(1), default=2)
+    ap.add_argument("--requests", type=at_least(1), default=8)
+    ap.add_argument("--prompt", type=at_least(1), default=16384, help="tokens of each request's prompt")
+    ap.add_argument("--chunk", type=at_least(1), default=4096, help="of which so many at a time")
+    ap.add_argument("--generate", type=at_least(0), default=64)
     ap.add_argument("--k-format", choices=sorted(mx.MX_FORMATS), default="e4m3")
     ap.add_argument("--v-format", choices=sorted(mx.MX_FORMATS), default="e4m3")
-    ap.add_argument("--read-blocks", type=int, default=0, help="blocks of 64 keys that a token reads (0: all)")
-    ap.add_argument("--page-keys", type=int, default=0)
+    ap.add_argument("--read-blocks", type=at_least(0), default=0, help="blocks of keys that a token reads (0: all keys)")
+    ap.add_argument("--block-keys", type=at_least(16), help="keys of a block: a power of two up to 4096, by default 64 or, if less, the page's")
+    ap.add_argument("--sink", type=at_least(0), help="first blocks that a token always reads, by default 1 where that leaves room for the newest")
+    ap.add_argument("--recent", type=at_least(0), help="newest blocks that a token always reads, by default 4 or, if less, what sink leaves")
+    ap.add_argument("--page-keys", type=at_least(0), default=0, help="keys of a page: a power of two from 16 on (0: slabs)")
     ap.add_argument("--seed", type=int, default=251114450)
-    a = ap.parse_args()
+    a = ap.parse_args(argv)
+    power_of_two = lambda v: v & (v - 1) == 0  # noqa: E731
+    if a.page_keys and (a.page_keys < 16 or not power_of_two(a.page_keys)):
+        ap.error("--page-keys: need a power of two from 16 on")
+    if a.block_keys is None:
+        a.block_keys = min(64, a.page_keys or 64)
+    if a.block_keys > (a.page_keys or 4096) or a.block_keys > 4096 or not power_of_two(a.block_keys):
+        ap.error("--block-keys: need a power of two from 16 to 4096 that divides --page-keys")
+    if a.sink is None:
+        a.sink = min(1, max(0, a.read_blocks - (1 if a.recent is None else a.recent)))
+    if a.recent is None:
+        a.recent = min(4, max(0, a.read_blocks - a.sink))
+    if a.read_blocks and a.sink + a.recent > a.read_blocks:
+        ap.error("--sink and --recent: need no more than --read-blocks together")
+    return a
+
+
+def main():
+    from .chain import MODELS, _Shape, _synthetic_layer
+    a = _arguments(sorted(MODELS))
     shape = _Shape(MODELS[a.model])
     make = _synthetic_layer(shape, a.seed)
     layers = [make(l) for l in range(a.blocks)]
     gen = torch.Generator(device="cuda")
     gen.manual_seed(a.seed + 13)
     draw = lambda rows: torch.randn((rows, shape.hidden), generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
-    blocks = LongBlocks(shape, layers, a.requests, a.prompt + a.generate, a.k_format, a.v_format, a.read_blocks, page_keys=a.page_keys)
+    blocks = LongBlocks(shape, layers, a.requests, a.prompt + a.generate, a.k_format, a.v_format, a.read_blocks, a.block_keys, a.sink, a.recent,
+                        a.page_keys)
     chunks = [min(a.chunk, a.prompt - at) for at in range(0, a.prompt, a.chunk)]
     inputs = [draw(a.requests * n) for n in chunks]
 
@@ -175,10 +204,11 @@ def main():
         torch.cuda.synchronize()
         return t1 - t0, time.perf_counter() - t1
 
-    run(2)
+    run(min(2, a.generate))  # there is room for no more
     prompt, tokens = run(a.generate)
     print(json.dumps(dict(model=a.model, blocks=a.blocks, requests=a.requests, prompt=a.prompt, generate=a.generate, k_format=a.k_format, v_format=a.v_format,
-                          read_blocks=a.read_blocks, prompt_ms=prompt * 1e3, token_ms=tokens * 1e3 / max(a.generate, 1), cache_mib=blocks.cache_bytes() / 2**20,
+                          read_blocks=a.read_blocks, block_keys=a.block_keys, sink=a.sink, recent=a.recent, prompt_ms=prompt * 1e3,
+                          token_ms=tokens * 1e3 / max(a.generate, 1), cache_mib=blocks.cache_bytes() / 2**20,
                           cache_mib_bf16=a.requests * (a.prompt + a.generate) * 4 * shape.n_kv_heads * shape.head_dim * a.blocks / 2**20)))
 
 
