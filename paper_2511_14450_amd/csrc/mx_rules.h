@@ -34,36 +34,59 @@ constexpr bool mx_token_two_tiles(int groups_of_features, bool f32) { return gro
 // mx_token: units of 32 keys, or of 16 where pages or listed blocks are so short, of a part, and parts of a request.
 constexpr int kMxMostUnits = 256;    // of a part: their places lie in LDS
 struct MxTokenPlan { int tiles, head_tiles, unit, units, parts; };  // tiles: of a wave; head_tiles: workgroups that share the heads; unit: log2 of its keys
+
+// Whether two workgroups have room on a CU; the kernels of float rows of more than 192 features take the registers of one.
+constexpr bool mx_token_two_workgroups(int groups_of_features, bool f32) { return !(f32 && groups_of_features > 6); }
+
+// Keys a us that go through a CU with one workgroup and with two, as far as a CU's 24 KB a us last.  Measured over 8 x 32768 keys of 8 KV heads (float
+// rows and 256 features: 4), less the 5 us of the join:
+//   bf16 rows     128 features, e2m1: 121, 147 (e4m3: bytes); 256 features, e2m1: 67, 70
+//   float rows    e4m3: 64 features 100, 138; 128 features 51, 76; 192 features 33, 47; 256 features 28
+//   two tiles     24 heads over one KV head of 8 x 131072 keys, 128 features: e4m3 58, 69; e2m1 58, 79
+struct MxTokenRates { int64_t alone, two; };
+inline MxTokenRates mx_token_rates(int64_t key_bytes, int groups_of_features, bool f32, bool two_tiles) {
+  const int64_t cu = 24000 / key_bytes, g = groups_of_features;
+  const MxTokenRates bf16 = {480 / std::max<int64_t>(g, 4), 590 / std::max<int64_t>(g, 4)};
+  const MxTokenRates r = two_tiles ? MxTokenRates{58, 74} : f32 ? MxTokenRates{std::min(204 / g, bf16.alone), std::min(300 / g, bf16.two)} : bf16;
+  return {std::min(cu, r.alone), std::min(cu, r.two)};
+}
+
 // Of one part a request, as many parts as give one workgroup a CU, and as many as give two, the one that a call is estimated to take the least time
-// with, by what was measured: a workgroup alone on a CU goes through 125 keys a us (f32 rows: 65) and two through 170 (85) together, as far
-// as a CU's 24 KB a us last; joining parts takes 6 us.  Eight heads of 8 x 32768 keys of 128 features: e4m3 in 256 / 512 workgroups 92 / 96 us,
-// e2m1 66 / 54, of 64 features 74 / 56; eight of 8 x 512 keys in one part 13, in two 18; ten heads of 24 x 2048 keys (e4m3, e2m1) in one part
-// 23, in two 29.  No part has fewer than 256 keys, and more workgroups than have room at once (2 a CU) wait for others to end.
+// with, by these rates and the longest part; joining parts takes 6 us.  Eight heads of 8 x 32768 keys of 128 features in 256 / 512 workgroups: e4m3
+// 90.7 / 95.1 us, e2m1 72.8 / 61, float rows over four heads 86 / 59, over four of 192 features 129 / 92; of 256 features and e2m1, which have no room for two a CU,
+// 105 / 112.  Eight heads of 8 x 512 keys in one part 10, in two 14; ten heads of 24 x 2048 keys (e4m3, e2m1) in one part 23.6, in two 29.5.
+// Parts are cut in whole multiples of eight units, and of 256 keys at least; the last one of a request has what is left.  More workgroups than have
+// room at once wait for others to end.
 //
-// Groups of more than 16 query heads go by two tiles of heads a wave where that still gives two workgroups a CU (one KV head of 8 x 131072 keys with 24
-// query heads: 75 us, by one tile 92; of 8 x 2000: 21.5 and 17).  pairs: of requests and KV heads
+// Groups of more than 16 query heads go by two tiles of heads a wave, by which keys are read and converted half as often and by half as many
+// workgroups, where 2048 parts of 256 keys, of eight requests' heads at least, are left: parts of fewer are more for the join, which has a workgroup for each
+// head.  24 heads over one KV head of 128 features, e4m3 / e2m1, by one tile and by two: 8 x 131072 keys 82 / 60 and 65 / 58 us, 64 x 8192
+// 57 / 43 and 44 / 39, 8 x 65536 47 / 38 and 43 / 38, 8 x 16384 20 / 19 and 24 / 22, 524288 of one request 50 / 47 and 62 / 59, 131072 25 / 28 and 45 / 44.
+// pairs: of requests and KV heads
 inline MxTokenPlan mx_token_plan(int64_t pairs, int group, int64_t keys, int64_t page_keys, int64_t block_keys, int64_t key_bytes, int groups_of_features, bool f32) {
   MxTokenPlan t = {};
-  const bool two_tiles = group > 16 && mx_token_two_tiles(groups_of_features, f32) && pairs * ((group + 31) / 32) * (keys / 256) >= 512;
+  const int64_t by_two = pairs * ((group + 31) / 32);
+  const bool two_tiles = group > 16 && mx_token_two_tiles(groups_of_features, f32) && by_two >= 8 && by_two * (keys / 256) >= 2048;
   t.tiles = two_tiles ? 2 : 1;
   t.head_tiles = (group + 16 * t.tiles - 1) / (16 * t.tiles);
   const int64_t items = pairs * t.head_tiles;
   t.unit = page_keys % 32 == 16 || block_keys == 16 ? 4 : 5;  // page_keys: also the room of a slab; block_keys: 0 where none are listed
   const int64_t units = (keys + (1 << t.unit) - 1) >> t.unit;
-  const int64_t cu = 24000 / key_bytes, alone = std::min<int64_t>(cu, two_tiles ? 45 : f32 ? 65 : 125), two = std::min<int64_t>(cu, two_tiles ? 80 : f32 ? 85 : 170);  // keys a us
-  int64_t parts = 1, least = 0;
+  const MxTokenRates rate = mx_token_rates(key_bytes, groups_of_features, f32, two_tiles);
+  const int64_t room = mx_token_two_workgroups(groups_of_features, f32) ? 512 : 256;
+  int64_t least = 0;
   for (int64_t places : {int64_t(0), int64_t(256), int64_t(512)}) {
+    if (places > room) continue;
     const int64_t n = std::max<int64_t>(1, std::min<int64_t>(places / items, keys / 256));
-    const int64_t time = (n * items <= 256 ? keys * 1000 / (n * alone) : keys * 2000 / (n * two)) + (n > 1 ? 6000 : 0);
+    const int64_t each = std::min<int64_t>(((units + n - 1) / n + 7) / 8 * 8, kMxMostUnits), parts = (units + each - 1) / each;
+    const int64_t workgroups = items * parts, rounds = (workgroups + room - 1) / room, of_two = workgroups > 256 && room == 512;
+    const int64_t longest = std::min(keys, each << t.unit), time = longest * 1000 * rounds * (of_two ? 2 : 1) / (of_two ? rate.two : rate.alone) + (parts > 1 ? 6000 : 0);
     if (places == 0 || time < least) {
-      parts = n;
+      t.units = (int)each;
+      t.parts = (int)parts;
       least = time;
     }
   }
-  int64_t each = (units + parts - 1) / parts;
-  each = std::min<int64_t>((each + 7) / 8 * 8, kMxMostUnits);
-  t.units = (int)each;
-  t.parts = (int)((units + each - 1) / each);
   return t;
 }
 

@@ -424,7 +424,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 
 // One part of a request's keys, of one KV head and up to 16 HT of its query heads: the waves take pairs of runs in turn, and join what they have in
 // LDS.
-template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && G > 6 ? 1 : 2) k_mx_token(const MxTokenCall p) {
+template <typename T, int G, int KF, int VF, int HT> __global__ void __launch_bounds__(kThreads, mx_token_two_workgroups(G, sizeof(T) == 4) ? 2 : 1) k_mx_token(const MxTokenCall p) {
   using Tk = Token<T, G, KF, VF, HT>;
   extern __shared__ char lds[];
   __shared__ int held[kWaves];           // units up to the last one that holds keys, among each wave's

@@ -31,12 +31,12 @@ def check(pr, q, scale, blocks=None):
 
 
 @pytest.mark.parametrize("formats", [("e4m3", "e4m3"), ("e4m3", "e2m1"), ("e2m1", "e4m3"), ("e2m1", "e2m1")])
-@pytest.mark.parametrize("heads,most", [(1, None), (17, None), (24, 132000)])  # the last by two tiles of heads a wave, in parts
+@pytest.mark.parametrize("heads,most", [(1, None), (17, None), (24, 70000)])  # the last by two tiles of heads a wave, in parts
 @pytest.mark.parametrize("d", [32, 128])
 def test_values_that_cancel_leave_what_the_probabilities_differ_by(d, heads, most, formats):
     # keys of probability 1 and values of 1 alternate with keys of 0.5 (1 + x) and values of -2: of each pair -x is left, which is less than half a
     # step of a bf16 beside 0.5
-    held = [64, 1000, 3000]
+    held = [64, 1000, 3000] + ([5, 300, 1, 0, 32] if most else [])
     pr = Problem(31, held, nkv=1, d=d, formats=formats, dtype=BF, block=0, layout="pages", page=1024, most=most)
     for b, n in enumerate(held):
         odd = (torch.arange(n) % 2).to(BF)
@@ -44,7 +44,7 @@ def test_values_that_cancel_leave_what_the_probabilities_differ_by(d, heads, mos
         pr.rows_k[b][:, 0, 0] = odd
         pr.rows_v[b] = (1 - 3 * odd)[:, None, None].expand(n, 1, d).contiguous()
     pr.fill()
-    q = torch.zeros((3, heads, d), dtype=BF)
+    q = torch.zeros((len(held), heads, d), dtype=BF)
     q[:, :, 0] = -1.0
     for x in (0.9 * 2.0 ** -8, 0.4 * 2.0 ** -8, -0.4 * 2.0 ** -8):
         check(pr, q, math.log(2.0) - math.log1p(x))
