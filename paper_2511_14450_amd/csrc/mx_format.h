@@ -16,8 +16,6 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ int mx_clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
 __device__ __forceinline__ int mx_len(const hyp_mx_cache_t &c, int b) { return mx_clamped(c.lens[b], 0, c.most); }
 
-constexpr int mx_bytes(int format) { return format == HYP_E4M3 ? 32 : 16; }  // of a group
-
 __device__ __forceinline__ float mx_scale(unsigned byte) { return __uint_as_float(byte << 23); }  // 0: the conversions take an exponent of -127; 255: NaN
 
 // numbers 2 p and 2 p + 1 of the eight that lie in word(s) w, as two bf16
