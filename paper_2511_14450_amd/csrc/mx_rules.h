@@ -16,8 +16,8 @@ inline int64_t mx_write_tiles(int64_t rows, int64_t requests, int64_t block, boo
 // mx_select: in one launch up to so many blocks of a request, or where all are kept.
 constexpr int kMxSmallBlocks = 256;
 inline bool mx_select_once(int blocks, int keep) { return blocks <= kMxSmallBlocks || blocks <= keep; }
-// Up to so many blocks are chosen among by 512 threads, which hold them in registers, more by 1024 (64 caches of up to 2048: 23.5 us, 25.3 with 1024;
-// 16 of 7813: 35, 38 with 512).
+// Up to so many blocks are chosen among by 512 threads, which hold them in registers, more by 1024 (64 caches of up to 2048: 22.7 us, 24.5 with 1024;
+// 16 of 7813: 33, 37 with 512).
 constexpr int kMxChooseBlocks = 2048;
 // Scores are formed by workgroups of 64 blocks once to four times: a row is converted once for all of them, but there have to be two workgroups
 // a CU.
@@ -53,13 +53,14 @@ inline MxTokenRates mx_token_rates(int64_t key_bytes, int groups_of_features, bo
 
 // Of one part a request, as many parts as give one workgroup a CU, and as many as give two, the one that a call is estimated to take the least time
 // with, by these rates and the longest part; joining parts takes 6 us.  Eight heads of 8 x 32768 keys of 128 features in 256 / 512 workgroups: e4m3
-// 90.7 / 95.1 us, e2m1 72.8 / 61, float rows over four heads 86 / 59, over four of 192 features 129 / 92; of 256 features and e2m1, which have no room for two a CU,
-// 105 / 112.  Eight heads of 8 x 512 keys in one part 10, in two 14; ten heads of 24 x 2048 keys (e4m3, e2m1) in one part 23.6, in two 29.5.
+// 90.7 / 95.1 us, e2m1 72.8 / 61, float rows over four heads 86 / 59, over four of 192 features 129 / 92; of 256 features and e2m1, which have no room
+// for two a CU, 105 / 112.  Eight heads of 8 x 512 keys in one part 10, in two 14; ten heads of 24 x 2048 keys (e4m3, e2m1) in one part 23.6, in two 29.5.
 // Parts are cut in whole multiples of eight units, and of 256 keys at least; the last one of a request has what is left.  More workgroups than have
 // room at once wait for others to end.
 //
 // Groups of more than 16 query heads go by two tiles of heads a wave, by which keys are read and converted half as often and by half as many
-// workgroups, where 2048 parts of 256 keys, of eight requests' heads at least, are left: parts of fewer are more for the join, which has a workgroup for each
+// workgroups, where pairs and two tiles of their heads are eight at least and have 2048 times 256 keys together: of fewer, each has more parts, and the join
+// has one workgroup for a query
 // head.  24 heads over one KV head of 128 features, e4m3 / e2m1, by one tile and by two: 8 x 131072 keys 82 / 60 and 65 / 58 us, 64 x 8192
 // 57 / 43 and 44 / 39, 8 x 65536 47 / 38 and 43 / 38, 8 x 16384 20 / 19 and 24 / 22, 524288 of one request 50 / 47 and 62 / 59, 131072 25 / 28 and 45 / 44.
 // pairs: of requests and KV heads

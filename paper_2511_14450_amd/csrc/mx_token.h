@@ -10,12 +10,13 @@
 // the sum of two, which hold it to 2^-16: as one, results were 2.0e-3 from the formula in 64 bits where rounding the results to bf16 costs
 // 1.6e-3 - 1.7e-3, and sums in which values cancel were off by as much as their terms' 2^-8.
 //
-// Bytes bound 8 bits: 8 x 32768 keys of 8 heads of 128 features, scores capped and falling with the distance, 92 us, of which the keys take 86 - 88 (6.3 -
-// 6.4 TB/s; a streaming read reaches 6.45) and the join 4.8.  4 bits have half as many and are bound by the issue of instructions and by waiting: 54 us,
-// 5.3 TB/s.  What it took: no clamped places in the loop (whole runs lie in the room; lengths count where codes are used), bytes to a unit of keys
-// in LDS, where 64-bit products on the scalar unit were (together 105 -> 96), streaming loads (-7 us; a cache that fits the memory-side one, of
-// 19 MB, takes 1 us more), the next pair of runs requested before one is worked on (4 bits: 59 -> 54; without it, at four waves a SIMD, 8 bits
-// are as fast), one workgroup a CU for 8 bits.  Eight waves a workgroup were slower (32 requests of 101 - 608 keys: 18.7 instead of 12).
+// Bytes bound 8 bits: 8 x 32768 keys of 8 heads of 128 features 90.5 us, of which the keys take 86 (6.4 TB/s; a streaming read reaches 6.45) and the
+// join 4.8; capped scores that fall with the distance make it 95.  4 bits have half as many and are bound by the issue of instructions and by waiting:
+// 58 us, 68 capped.  What it took, in steps that were each measured over the capped ones with one bf16 a probability: no clamped places in the loop
+// (whole runs lie in the room; lengths count where codes are used), bytes to a unit of keys in LDS, where 64-bit products on the scalar unit were
+// (together 105 -> 96), streaming loads (-7 us; a cache that fits the memory-side one, of 19 MB, takes 1 us more), the next pair of runs requested before
+// one is worked on (4 bits: 59 -> 54; without it, at four waves a SIMD, 8 bits are as fast), one workgroup a CU for 8 bits.  Eight waves a workgroup
+// were slower (32 requests of 101 - 608 keys: 18.7 instead of 12).  Two bf16 a probability took 3 % (listed blocks) to 9 % (4 bits) more.
 #pragma once
 
 #include <atomic>
